@@ -14,3 +14,12 @@ from .binding import (  # noqa: F401
     lf_last_error, lf_destroy,
     LeapfrogNet,
 )
+from .operators import (  # noqa: F401
+    LF_MATRIX_F32, LF_MATRIX_BF16, LF_MATRIX_E4M3,
+    LF_ACT_NONE, LF_ACT_SIGMOID, LF_ACT_RELU, LF_ACT_SILU, LF_ACT_GELU,
+    lf_matrix, lf_checkpoint_save, lf_checkpoint_load, lf_norm_forward, lf_norm_workspace_bytes, lf_norm_backward,
+    lf_linear_workspace_bytes, lf_linear_forward, lf_linear_backward_workspace_bytes, lf_linear_backward,
+    lf_operator_error,
+    E4M3Matrix, RmsNorm, Linear,
+)
+from .residual_net import ResidualNet  # noqa: F401

@@ -12,7 +12,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblf.so")
-SOURCES = ["lf_api.hip", "b1_kernels.hip", "batched_kernels.hip", "persistent_kernels.hip"]
+SOURCES = ["lf_api.hip", "b1_kernels.hip", "batched_kernels.hip", "persistent_kernels.hip",
+           "operators_api.hip", "norm_kernels.hip", "product_kernels.hip"]
 OBJ_DIR = os.path.join(HERE, "_build")              # object files (not committed)
 ROOT = os.path.dirname(HERE)
 PROBE_LIB = os.path.join(ROOT, "libbench_probe.so")      # measurement aid of bench.py, not part of the library

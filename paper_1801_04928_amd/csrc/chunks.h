@@ -1,0 +1,153 @@
+// Chunks of eight consecutive values of a row, as the operators' kernels read and write them: from fp32, bf16, or 8 bits with
+// scales.  Four lanes with four neighbouring chunks hold one group of 32 values of a matrix in 8 bits.
+#pragma once
+#include "device_helpers.h"
+#include "operators_internal.h"
+
+namespace lf {
+namespace ops {
+
+constexpr int kGroup = 32;        // values that share a scale
+constexpr int kChunk = 8;
+
+// Vectors at any address of their elements: global memory takes wide loads and stores that are not aligned to their
+// width, so one instruction serves aligned rows and others (which cost the lines they straddle).
+typedef v4f any_v4f __attribute__((aligned(4)));
+typedef v8bf any_v8bf __attribute__((aligned(2)));
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+
+template <int KIND> struct Stored;
+template <> struct Stored<F32> { typedef float type; };
+template <> struct Stored<BF16> { typedef __bf16 type; };
+
+template <class T> using global_ptr = T __attribute__((address_space(1)))*;
+template <class T, class U> __device__ __forceinline__ global_ptr<T> as_global(U* p) { return (global_ptr<T>)(p); }
+
+// n (0..8) values from p; the others are zero.
+template <class T>
+__device__ __forceinline__ void load_values(const T* p, int n, float (&v)[8]) {
+    if (n >= kChunk) {
+        if constexpr (sizeof(T) == 4) {
+            const v4f a = *as_global<const any_v4f>(p), b = *as_global<const any_v4f>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        } else {
+            const v8bf a = *as_global<const any_v8bf>(p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)*as_global<const T>(p + i) : 0.0f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_values(T* p, int n, const float (&v)[8]) {
+    if (n >= kChunk) {
+        if constexpr (sizeof(T) == 4) {
+            *as_global<any_v4f>(p) = v4f{v[0], v[1], v[2], v[3]};
+            *as_global<any_v4f>(p + 4) = v4f{v[4], v[5], v[6], v[7]};
+        } else {
+            v8bf a;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = (__bf16)v[i];
+            *as_global<any_v8bf>(p) = a;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) *as_global<T>(p + i) = (T)v[i];
+    }
+}
+
+// ---- 8 bits ----------------------------------------------------------------------------------------------------------
+// The scale of a group whose largest finite magnitude is m, as e + 127: the least e >= -117 with m <= 448 2^e.  448 is 1.75 2^8,
+// so e is m's exponent less 8, one more if its significand is above 1.75: the addition carries into the exponent then.
+__device__ __forceinline__ int scale_byte(float m) {
+    const int e = (int)((__float_as_uint(m) + 0x1FFFFFu) >> 23) - 8;
+    return e < 10 ? 10 : e;
+}
+__device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((unsigned)byte << 23); }
+__device__ __forceinline__ float finite_magnitude(float v) {
+    const float a = fabsf(v);
+    return a < __builtin_inff() ? a : 0.0f;          // NaN and infinities do not set a scale
+}
+// Largest of the four lanes of a quad (all of them active).
+__device__ __forceinline__ float quad_max(float m) {
+    m = fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, m), 0xB1, 0xF, 0xF, true)));
+    return fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, m), 0x4E, 0xF, 0xF, true)));
+}
+// One value in units of its group's scale, ready for the conversion (which rounds to nearest even).
+__device__ __forceinline__ float scaled_value(float v, float inverse, float most) {
+    const float s = fminf(fmaxf(v * inverse, -most), most);
+    return fabsf(v) < __builtin_inff() ? s : __builtin_nanf("");
+}
+__device__ __forceinline__ v2u eight_codes(const float (&v)[8], int byte) {
+    const float inverse = scale_value(254 - byte);
+    const float most = byte == 247 ? 240.0f : 448.0f;          // 256 * 2^120 would be no finite number
+    int w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int r = 0;
+        r = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_value(v[4 * h], inverse, most), scaled_value(v[4 * h + 1], inverse, most), r, false);
+        r = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_value(v[4 * h + 2], inverse, most), scaled_value(v[4 * h + 3], inverse, most), r, true);
+        w[h] = r;
+    }
+    return v2u{(unsigned)w[0], (unsigned)w[1]};
+}
+// Chunk `col` (a multiple of 8) of a row in 8 bits.  The four lanes of a quad hold the four chunks of a group and all call this;
+// values past the last column are zero.  live: the chunk's group begins inside the row, so its memory is there.
+__device__ __forceinline__ void store_eight(uint8_t* codes, uint8_t* scales, int col, const float (&v)[8], bool live) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_magnitude(v[i]));
+    const int byte = scale_byte(quad_max(m));
+    const v2u w = eight_codes(v, byte);
+    if (live) {
+        *as_global<v2u>(codes + col) = w;
+        if (col % kGroup == 0) *as_global<uint8_t>(scales + col / kGroup) = (uint8_t)byte;
+    }
+}
+// The values of eight codes.
+__device__ __forceinline__ void eight_values(v2u w, float scale, float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], true);
+        v[4 * h] = a[0] * scale;
+        v[4 * h + 1] = a[1] * scale;
+        v[4 * h + 2] = b[0] * scale;
+        v[4 * h + 3] = b[1] * scale;
+    }
+}
+
+// Values col .. col + n - 1 of a row (n <= 8; n <= 0: none), the others zero; col is a multiple of 8.
+template <int KIND>
+__device__ __forceinline__ void load_chunk(const Mat& m, long long row, int col, int n, float (&v)[8]) {
+    if constexpr (KIND == E4M3) {
+        if (n > 0) {
+            const v2u w = *as_global<const v2u>((const uint8_t*)m.p + row * m.ld + col);
+            eight_values(w, scale_value(*as_global<const uint8_t>(m.scales + row * m.scale_ld + col / kGroup)), v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.0f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        }
+    } else {
+        typedef typename Stored<KIND>::type T;
+        load_values((const T*)m.p + row * m.ld + col, n, v);
+    }
+}
+// All lanes call this (see store_eight); live: the row is there and col < the row's columns rounded up to whole groups.
+template <int KIND>
+__device__ __forceinline__ void store_chunk(const Mat& m, long long row, int col, int n, const float (&v)[8], bool live) {
+    if constexpr (KIND == E4M3) {
+        store_eight((uint8_t*)m.p + row * m.ld, m.scales + row * m.scale_ld, col, v, live);
+    } else {
+        typedef typename Stored<KIND>::type T;
+        if (live && n > 0) store_values((T*)m.p + row * m.ld + col, n, v);
+    }
+}
+
+}  // namespace ops
+}  // namespace lf
