@@ -120,6 +120,92 @@ __device__ __forceinline__ void eight_values(v2u w, float scale, float (&v)[8]) 
     }
 }
 
+// ---- chunks on their way --------------------------------------------------------------------------------------------------
+// Elements move down by s places (s >= 8: zeros).
+__device__ __forceinline__ void shift_down(v4u& a, int s) {                 // eight of 16 bits
+    v4u b = (s & 4) ? v4u{a[2], a[3], 0u, 0u} : a;
+    b = (s & 2) ? v4u{b[1], b[2], b[3], 0u} : b;
+    const v4u h = {b[0] >> 16 | b[1] << 16, b[1] >> 16 | b[2] << 16, b[2] >> 16 | b[3] << 16, b[3] >> 16};
+    b = (s & 1) ? h : b;
+    a = s < 8 ? b : v4u{0u, 0u, 0u, 0u};
+}
+__device__ __forceinline__ void shift_down(v4f (&a)[2], int s) {            // eight of 32 bits
+    const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (s & 4) { a[0] = a[1]; a[1] = zero; }
+    if (s & 2) { a[0] = v4f{a[0][2], a[0][3], a[1][0], a[1][1]}; a[1] = v4f{a[1][2], a[1][3], 0.0f, 0.0f}; }
+    if (s & 1) { a[0] = v4f{a[0][1], a[0][2], a[0][3], a[1][0]}; a[1] = v4f{a[1][1], a[1][2], a[1][3], 0.0f}; }
+    if (s >= 8) a[0] = a[1] = zero;
+}
+// The first n of the codes stay, the others become zeros.
+template <class V>
+__device__ __forceinline__ void keep_codes(V& a, int n) {
+#pragma unroll
+    for (int w = 0; w < (int)(sizeof(V) / 4); ++w) {
+        const int k = n - 4 * w;
+        a[w] &= k >= 4 ? ~0u : k <= 0 ? 0u : (1u << (8 * k)) - 1u;
+    }
+}
+
+// A chunk as it was loaded.  Loads have no branch around them, so that many are under way: a chunk that the row's end cuts is
+// loaded from as far ahead as makes it whole, one past the end from the row's last eight, and both are put right when
+// the values are taken.  That needs rows of eight values; NARROW is for fewer.
+template <int KIND> struct Chunk;
+template <> struct Chunk<F32> { v4f a[2]; };
+template <> struct Chunk<BF16> { v4u a; };
+template <> struct Chunk<E4M3> { v2u a; int byte; };
+
+// Chunk of the row (which is there) from column col on; cols: the matrix's columns.
+template <int KIND, bool NARROW>
+__device__ __forceinline__ void fetch_chunk(Chunk<KIND>& c, const Mat& m, long long row, int col, int cols) {
+    if constexpr (KIND == E4M3) {
+        const int at = min(col, (cols - 1) / kGroup * kGroup + (kGroup - kChunk));
+        c.a = *as_global<const v2u>((const uint8_t*)m.p + row * m.ld + at);
+        c.byte = *as_global<const uint8_t>(m.scales + row * m.scale_ld + at / kGroup);
+    } else {
+        typedef typename Stored<KIND>::type T;
+        const T* p = (const T*)m.p + row * m.ld;
+        if constexpr (NARROW) {
+            float v[8];
+            load_values(p + col, max(0, cols - col), v);
+            if constexpr (KIND == F32) {
+                c.a[0] = v4f{v[0], v[1], v[2], v[3]};
+                c.a[1] = v4f{v[4], v[5], v[6], v[7]};
+            } else {
+                v8bf b;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) b[i] = (__bf16)v[i];
+                c.a = __builtin_bit_cast(v4u, b);
+            }
+        } else {
+            p += min(col, cols - kChunk);
+            if constexpr (KIND == F32) {
+                c.a[0] = *as_global<const any_v4f>(p);
+                c.a[1] = *as_global<const any_v4f>(p + 4);
+            } else {
+                c.a = __builtin_bit_cast(v4u, *as_global<const any_v8bf>(p));
+            }
+        }
+    }
+}
+// Its values; n (0..8) of them are in the row, the others are zero.
+template <int KIND, bool NARROW>
+__device__ __forceinline__ void take_chunk(Chunk<KIND> c, int n, float (&v)[8]) {
+    if (n < kChunk) {
+        if constexpr (KIND == E4M3) keep_codes(c.a, n);
+        else if constexpr (!NARROW) shift_down(c.a, kChunk - max(n, 0));
+    }
+    if constexpr (KIND == E4M3) {
+        eight_values(c.a, scale_value(c.byte), v);
+    } else if constexpr (KIND == F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = c.a[0][i]; v[4 + i] = c.a[1][i]; }
+    } else {
+        const v8bf b = __builtin_bit_cast(v8bf, c.a);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)b[i];
+    }
+}
+
 // Values col .. col + n - 1 of a row (n <= 8; n <= 0: none), the others zero; col is a multiple of 8.
 template <int KIND>
 __device__ __forceinline__ void load_chunk(const Mat& m, long long row, int col, int n, float (&v)[8]) {

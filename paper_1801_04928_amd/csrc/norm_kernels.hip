@@ -5,6 +5,7 @@
 #include "chunks.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lf {
 namespace ops {
@@ -53,41 +54,42 @@ __device__ __forceinline__ void load_gain(const float* gain, int col, int n, flo
 
 // TPR threads hold a row, NCH chunks of eight values each: a row is read once.  AGAIN: rows wider than TPR * NCH chunks are
 // read a second time for the outputs.
-template <int T, int OUT, int TPR, int NCH, bool AGAIN>
+template <int T, int OUT, int TPR, int NCH, bool AGAIN, bool NARROW>
 __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_norm_forward(const NormForward a) {
     constexpr int kRows = TPR > kThreads ? 1 : kThreads / TPR;
     __shared__ float shared[TPR > kWave ? TPR / kWave : 1];
     const int t = threadIdx.x % TPR;
     const bool more = a.branch.p != nullptr;
+    const int turns = AGAIN ? ceil_div(a.cols, kChunk * TPR * NCH) : 1;
     long long row;
 
-    auto load = [&](int chunk, float (&v)[8]) {
-        const int col = chunk * kChunk, n = a.cols - col;
-        load_chunk<T>(a.x, row, col, n, v);
-        if (more) {
-            float u[8];
-            load_chunk<T>(a.branch, row, col, n, u);
+    auto load = [&](int turn, float (&v)[NCH][8]) {
+        Chunk<T> x[NCH], branch[NCH];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += u[i];
+        for (int j = 0; j < NCH; ++j)
+            fetch_chunk<T, NARROW>(x[j], a.x, row, ((turn * NCH + j) * TPR + t) * kChunk, a.cols);
+        if (more) {
+#pragma unroll
+            for (int j = 0; j < NCH; ++j)
+                fetch_chunk<T, NARROW>(branch[j], a.branch, row, ((turn * NCH + j) * TPR + t) * kChunk, a.cols);
+        }
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int n = a.cols - ((turn * NCH + j) * TPR + t) * kChunk;
+            take_chunk<T, NARROW>(x[j], n, v[j]);
+            if (more) {
+                float u[8];
+                take_chunk<T, NARROW>(branch[j], n, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] += u[i];
+            }
         }
     };
-    auto store = [&](int chunk, const float (&v)[8], float rstd) {
-        const int col = chunk * kChunk, n = a.cols - col;
-        if (a.sum.p) store_chunk<T>(a.sum, row, col, n, v, n > 0);
-        float g[8], y[8];
-        load_gain(a.gain, col, n, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = i < n ? v[i] * rstd * g[i] : 0.0f;
-        store_chunk<OUT>(a.y, row, col, n, y, col < whole_groups(a.cols));
-    };
-
-    const int turns = AGAIN ? ceil_div(a.cols, kChunk * TPR * NCH) : 1;
     // (the grid has a block for every kRows rows, up to kMostGroups of them)
-    for (row = (long long)blockIdx.x * kRows + threadIdx.x / TPR; row < a.rows; row += (long long)gridDim.x * kRows) {
+    for (row = (long long)blockIdx.x * kRows + (kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR)); row < a.rows; row += (long long)gridDim.x * kRows) {
         float v[NCH][8], square = 0.0f;
         for (int turn = 0; turn < turns; ++turn) {
-#pragma unroll
-            for (int j = 0; j < NCH; ++j) load((turn * NCH + j) * TPR + t, v[j]);
+            load(turn, v);
 #pragma unroll
             for (int j = 0; j < NCH; ++j)
 #pragma unroll
@@ -96,12 +98,17 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_norm_forwar
         const float rstd = 1.0f / sqrtf(row_sum<TPR>(square, shared) / (float)a.cols + a.eps);
         if (a.rstd && t == 0) a.rstd[row] = rstd;
         for (int turn = 0; turn < turns; ++turn) {
-            if constexpr (AGAIN) {
+            if constexpr (AGAIN) load(turn, v);
 #pragma unroll
-                for (int j = 0; j < NCH; ++j) load((turn * NCH + j) * TPR + t, v[j]);
+            for (int j = 0; j < NCH; ++j) {
+                const int col = ((turn * NCH + j) * TPR + t) * kChunk, n = a.cols - col;
+                if (a.sum.p) store_chunk<T>(a.sum, row, col, n, v[j], n > 0);
+                float g[8], y[8];
+                load_gain(a.gain, col, n, g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = i < n ? v[j][i] * rstd * g[i] : 0.0f;
+                store_chunk<OUT>(a.y, row, col, n, y, col < whole_groups(a.cols));
             }
-#pragma unroll
-            for (int j = 0; j < NCH; ++j) store((turn * NCH + j) * TPR + t, v[j], rstd);
         }
     }
 }
@@ -118,65 +125,102 @@ struct NormBackward {
 };
 
 // A block takes rows blockIdx.x, + gridDim.x, ...: the sums of dy h over its rows stay in registers, a row of partial sums
-// per block is all that the gain's gradient costs in memory.  AGAIN as in the forward pass (the gain's gradient is then
-// a kernel of its own, k_gain_gradient).
-template <int T, int S, int TPR, int NCH, bool AGAIN>
+// per block is all that the gain's gradient costs in memory.  The next row is under way, as it lies in memory, while one is
+// worked on.  AGAIN as in the forward pass (the gain's gradient is then a kernel of its own, k_gain_gradient).
+template <int T, int S, int TPR, int NCH, bool AGAIN, bool NARROW>
 __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_norm_backward(const NormBackward a) {
     constexpr int kBlock = TPR > kThreads ? TPR : kThreads, kRows = kBlock / TPR;
     __shared__ float shared[TPR > kWave ? TPR / kWave : 1];
-    const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR;
-    float total[AGAIN ? 1 : NCH][8];
+    // (the row is the same for a whole wave: its addresses are scalars)
+    const int t = threadIdx.x % TPR, mine = kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    const bool more = a.dsum.p != nullptr;
+    const long long step = (long long)gridDim.x * kRows;
+    const auto col_of = [&](int turn, int j) { return ((turn * NCH + j) * TPR + t) * kChunk; };
+    float total[AGAIN ? 1 : NCH][8], gain[AGAIN ? 1 : NCH][8];
+    Chunk<T> dy_raw[NCH], dsum_raw[NCH];
+    Chunk<S> s_raw[NCH];
+    float rstd_raw = 0.0f;
+    auto request = [&](long long row, int turn) {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            fetch_chunk<T, NARROW>(dy_raw[j], a.dy, row, col_of(turn, j), a.cols);
+            fetch_chunk<S, NARROW>(s_raw[j], a.sum, row, col_of(turn, j), a.cols);
+        }
+        rstd_raw = a.rstd[row];
+    };
+    auto request_dsum = [&](long long row, int turn) {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) fetch_chunk<T, NARROW>(dsum_raw[j], a.dsum, row, col_of(turn, j), a.cols);
+    };
+    // t = dy gain and h = sum rstd of chunk j
+    auto take = [&](int turn, int j, float rstd, float (&dy)[8], float (&h)[8]) {
+        const int n = a.cols - col_of(turn, j);
+        take_chunk<T, NARROW>(dy_raw[j], n, dy);
+        take_chunk<S, NARROW>(s_raw[j], n, h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] *= rstd;
+    };
     if constexpr (!AGAIN) {
 #pragma unroll
-        for (int j = 0; j < NCH; ++j)
+        for (int j = 0; j < NCH; ++j) {
+            load_gain(a.gain, col_of(0, j), a.cols - col_of(0, j), gain[j]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) total[j][i] = 0.0f;
+        }
     }
-    for (long long row = (long long)blockIdx.x * kRows + mine; row < a.rows; row += (long long)gridDim.x * kRows) {
-        const float rstd = a.rstd[row];
+    long long row = (long long)blockIdx.x * kRows + mine;
+    if constexpr (!AGAIN) {
+        if (row < a.rows) request(row, 0);
+    }
+    for (; row < a.rows; row += step) {
         float dy[NCH][8], h[NCH][8], along = 0.0f;
         const int turns = AGAIN ? ceil_div(a.cols, kChunk * TPR * NCH) : 1;
-        for (int turn = 0; turn < turns; ++turn) {
+        if constexpr (AGAIN) {
+            for (int turn = 0; turn < turns; ++turn) {
+                request(row, turn);
 #pragma unroll
-            for (int j = 0; j < NCH; ++j) {
-                const int col = ((turn * NCH + j) * TPR + t) * kChunk, n = a.cols - col;
-                load_chunk<T>(a.dy, row, col, n, dy[j]);
-                load_chunk<S>(a.sum, row, col, n, h[j]);
+                for (int j = 0; j < NCH; ++j) {
+                    float g[8];
+                    take(turn, j, rstd_raw, dy[j], h[j]);
+                    load_gain(a.gain, col_of(turn, j), a.cols - col_of(turn, j), g);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) along = fmaf(dy[j][i] * g[i], h[j][i], along);
+                }
             }
+        } else {
+            if (more) request_dsum(row, 0);
 #pragma unroll
             for (int j = 0; j < NCH; ++j) {
-                const int col = ((turn * NCH + j) * TPR + t) * kChunk, n = a.cols - col;
-                float g[8];
-                load_gain(a.gain, col, n, g);
+                take(0, j, rstd_raw, dy[j], h[j]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    h[j][i] *= rstd;
-                    if constexpr (!AGAIN) total[j][i] = fmaf(dy[j][i], h[j][i], total[j][i]);
-                    dy[j][i] *= g[i];
+                    total[j][i] = fmaf(dy[j][i], h[j][i], total[j][i]);
+                    dy[j][i] *= gain[j][i];
                     along = fmaf(dy[j][i], h[j][i], along);
                 }
             }
         }
+        const float rstd = rstd_raw;
+        // (past the last row the last one again: no branch around the loads)
+        if constexpr (!AGAIN) request(min(row + step, (long long)a.rows - 1), 0);
         const float mean = row_sum<TPR>(along, shared) / (float)a.cols;
         for (int turn = 0; turn < turns; ++turn) {
+            if constexpr (AGAIN) {
+                request(row, turn);
+                if (more) request_dsum(row, turn);
+            }
 #pragma unroll
             for (int j = 0; j < NCH; ++j) {
-                const int col = ((turn * NCH + j) * TPR + t) * kChunk, n = a.cols - col;
+                const int col = col_of(turn, j), n = a.cols - col;
                 if constexpr (AGAIN) {
                     float g[8];
-                    load_chunk<T>(a.dy, row, col, n, dy[j]);
-                    load_chunk<S>(a.sum, row, col, n, h[j]);
+                    take(turn, j, rstd, dy[j], h[j]);
                     load_gain(a.gain, col, n, g);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) { h[j][i] *= rstd; dy[j][i] *= g[i]; }
+                    for (int i = 0; i < 8; ++i) dy[j][i] *= g[i];
                 }
-                float d[8];
-                if (a.dsum.p) {
-                    load_chunk<T>(a.dsum, row, col, n, d);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = 0.0f;
-                }
+                float d[8] = {};
+                if (more) take_chunk<T, NARROW>(dsum_raw[j], n, d);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, dy[j][i] - h[j][i] * mean, d[i]);
                 store_chunk<T>(a.dx, row, col, n, d, n > 0);
@@ -188,23 +232,21 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_norm_backwa
         float* out = a.partial + (size_t)blockIdx.x * a.cols;
         if constexpr (kRows == 1) {
 #pragma unroll
-            for (int j = 0; j < NCH; ++j) {
-                const int col = (j * TPR + t) * kChunk;
-                if (col < a.cols) store_values(out + col, a.cols - col, total[j]);
-            }
+            for (int j = 0; j < NCH; ++j)
+                if (col_of(0, j) < a.cols) store_values(out + col_of(0, j), a.cols - col_of(0, j), total[j]);
         } else {
             __shared__ float rows_total[kRows - 1][NCH * TPR * kChunk];
             if (mine > 0) {
 #pragma unroll
                 for (int j = 0; j < NCH; ++j)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) rows_total[mine - 1][(j * TPR + t) * kChunk + i] = total[j][i];
+                    for (int i = 0; i < 8; ++i) rows_total[mine - 1][col_of(0, j) + i] = total[j][i];
             }
             __syncthreads();
             if (mine == 0) {
 #pragma unroll
                 for (int j = 0; j < NCH; ++j) {
-                    const int col = (j * TPR + t) * kChunk;
+                    const int col = col_of(0, j);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -254,33 +296,67 @@ __global__ __launch_bounds__(kThreads) void k_gain_gradient(const NormBackward a
     strip_finish(total, a.partial, a.cols);
 }
 
+template <int ACT>
+__device__ __forceinline__ void times_slope(float (&d)[8], const float (&z)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] *= slope(ACT, z[i]);
+}
+
 // ================================================================================================
 // the gradient before an activation, and its sums over rows
 // ================================================================================================
+// A block is W chunks wide and kThreads / W rows high and walks down a part of the rows, kSlopeSteps of its heights at once.  Four
+// chunks where one part holds all rows (its sums are db itself): of few values, the more threads the less each
+// computes.  16 chunks, whole lines, where memory counts.
+constexpr int kSlopeSteps = 2, kNarrowStrip = 4, kWideStrip = 16;
 struct Slope {
     int rows, cols, act;
     Mat dy, z, dz;
     float* partial;      // [gridDim.y][cols], or null
 };
-template <int T, int Z>
+template <int T, int Z, int W>
 __global__ __launch_bounds__(kThreads) void k_slope(const Slope a, int rows_per_block) {
-    const int col = (blockIdx.x * kStripChunks + threadIdx.x % kStripChunks) * kChunk, n = a.cols - col;
+    constexpr int kHigh = kThreads / W;
+    const int t = threadIdx.x % W, mine = threadIdx.x / W;
+    const int col = (blockIdx.x * W + t) * kChunk, n = a.cols - col;
     const int first = blockIdx.y * rows_per_block, end = min(a.rows, first + rows_per_block);
     float total[8] = {};
-    for (int row = first + threadIdx.x / kStripChunks; row < end; row += kStripRows) {
-        float d[8];
-        load_chunk<T>(a.dy, row, col, n, d);
-        if (a.act != NONE) {
-            float z[8];
-            load_chunk<Z>(a.z, row, col, n, z);
+    for (int row0 = first + mine; row0 < end; row0 += kHigh * kSlopeSteps) {
+        float d[kSlopeSteps][8], z[kSlopeSteps][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] *= slope(a.act, z[i]);
+        for (int u = 0; u < kSlopeSteps; ++u) {
+            const int row = row0 + u * kHigh, there = row < end ? n : 0;
+            load_chunk<T>(a.dy, row, col, there, d[u]);
+            if (a.act != NONE) load_chunk<Z>(a.z, row, col, there, z[u]);
         }
-        if (a.dz.p) store_chunk<T>(a.dz, row, col, n, d, n > 0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) total[i] += d[i];
+        for (int u = 0; u < kSlopeSteps; ++u) {
+            const int row = row0 + u * kHigh;
+            if (row >= end) continue;
+            switch (a.act) {
+                case SIGMOID: times_slope<SIGMOID>(d[u], z[u]); break;
+                case RELU: times_slope<RELU>(d[u], z[u]); break;
+                case SILU: times_slope<SILU>(d[u], z[u]); break;
+                case GELU: times_slope<GELU>(d[u], z[u]); break;
+                default: break;
+            }
+            if (a.dz.p) store_chunk<T>(a.dz, row, col, n, d[u], n > 0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) total[i] += d[u][i];
+        }
     }
-    if (a.partial) strip_finish(total, a.partial, a.cols);
+    if (!a.partial) return;
+    __shared__ float others[kHigh][W * kChunk + 1];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) others[mine][t * kChunk + i] = total[i];
+    __syncthreads();
+    const int c = threadIdx.x, out = blockIdx.x * W * kChunk + c;
+    if (c < W * kChunk && out < a.cols) {
+        float v = others[0][c];
+#pragma unroll 8
+        for (int r = 1; r < kHigh; ++r) v += others[r][c];
+        a.partial[(size_t)blockIdx.y * a.cols + out] = v;
+    }
 }
 
 // Sums of partial rows: 64 columns a block, 16 threads a column, each over every sixteenth row.
@@ -344,35 +420,38 @@ hipError_t copy(int rows, int cols, const Mat& from, const Mat& to, hipStream_t 
     return hipGetLastError();
 }
 
-// Threads and chunks a row takes: the fewest chunks a thread that hold it, waves of their own up to 2048 columns.
+// Threads that hold a row, each NCH chunks of it.  Waves of their own up to 1024 columns: no barrier.
 template <class F> hipError_t by_width(int cols, F&& f) {
     using std::integral_constant;
-    if (cols <= 512) return f(integral_constant<int, 64>(), integral_constant<int, 1>(), std::false_type());
-    if (cols <= 1024) return f(integral_constant<int, 64>(), integral_constant<int, 2>(), std::false_type());
-    if (cols <= 2048) return f(integral_constant<int, 64>(), integral_constant<int, 4>(), std::false_type());
-    if (cols <= 4096) return f(integral_constant<int, 256>(), integral_constant<int, 2>(), std::false_type());
-    if (cols <= 8192) return f(integral_constant<int, 256>(), integral_constant<int, 4>(), std::false_type());
-    if (cols <= 16384) return f(integral_constant<int, 512>(), integral_constant<int, 4>(), std::false_type());
-    return f(integral_constant<int, 512>(), integral_constant<int, 4>(), std::true_type());
+    const std::false_type no;
+    const std::true_type yes;
+    const integral_constant<int, 2> two;
+    if (cols < kChunk) return f(integral_constant<int, 64>(), integral_constant<int, 1>(), no, yes);
+    if (cols <= 512) return f(integral_constant<int, 64>(), integral_constant<int, 1>(), no, no);
+    if (cols <= 1024) return f(integral_constant<int, 64>(), two, no, no);
+    if (cols <= 4096) return f(integral_constant<int, 256>(), two, no, no);
+    if (cols <= 8192) return f(integral_constant<int, 512>(), two, no, no);
+    if (cols <= 16384) return f(integral_constant<int, 1024>(), two, no, no);
+    return f(integral_constant<int, 1024>(), two, yes, no);
 }
 constexpr int kHeldCols = 16384;
-int rows_per_block(int cols) { return cols <= 2048 ? 4 : 1; }
+int rows_per_block(int cols) { return cols <= 1024 ? 4 : 1; }
 
 template <int T, int OUT>
 hipError_t norm_forward(const NormForward& a, hipStream_t s) {
-    return by_width(a.cols, [&](auto tpr, auto nch, auto again) {
+    return by_width(a.cols, [&](auto tpr, auto nch, auto again, auto narrow) {
         constexpr int block = tpr() > kThreads ? tpr() : kThreads;
-        k_norm_forward<T, OUT, tpr(), nch(), again()><<<dim3(std::min(ceil_div(a.rows, block / tpr()), kMostGroups)),
+        k_norm_forward<T, OUT, tpr(), nch(), again(), narrow()><<<dim3(std::min(ceil_div(a.rows, block / tpr()), kMostGroups)),
                                                             block, 0, s>>>(a);
         return hipGetLastError();
     });
 }
 template <int T, int S>
 hipError_t norm_backward(const NormBackward& a, hipStream_t s) {
-    return by_width(a.cols, [&](auto tpr, auto nch, auto again) {
+    return by_width(a.cols, [&](auto tpr, auto nch, auto again, auto narrow) {
         constexpr int block = tpr() > kThreads ? tpr() : kThreads;
         const int groups = again() ? std::min(a.rows, kMostGroups) : norm_partials(a.rows, a.cols);
-        k_norm_backward<T, S, tpr(), nch(), again()><<<dim3(groups), block, 0, s>>>(a);
+        k_norm_backward<T, S, tpr(), nch(), again(), narrow()><<<dim3(groups), block, 0, s>>>(a);
         if (again() && a.partial) {
             const int parts = norm_partials(a.rows, a.cols);
             k_gain_gradient<T, S><<<dim3(ceil_div(a.cols, kStripChunks * kChunk), parts), kThreads, 0, s>>>(
@@ -383,7 +462,9 @@ hipError_t norm_backward(const NormBackward& a, hipStream_t s) {
 }
 template <int T, int Z>
 hipError_t slopes(const Slope& a, int parts, hipStream_t s) {
-    k_slope<T, Z><<<dim3(ceil_div(a.cols, kStripChunks * kChunk), parts), kThreads, 0, s>>>(a, ceil_div(a.rows, parts));
+    const int rows = ceil_div(a.rows, parts);
+    if (parts == 1) k_slope<T, Z, kNarrowStrip><<<dim3(ceil_div(a.cols, kNarrowStrip * kChunk)), kThreads, 0, s>>>(a, rows);
+    else k_slope<T, Z, kWideStrip><<<dim3(ceil_div(a.cols, kWideStrip * kChunk), parts), kThreads, 0, s>>>(a, rows);
     return hipGetLastError();
 }
 
@@ -407,19 +488,23 @@ hipError_t launch_norm_forward(int rows, int cols, const Mat& x, const Mat& bran
 int norm_partials(int rows, int cols) {
     if (rows == 0) return 0;
     if (cols > kHeldCols) return std::min(ceil_div(rows, 16), 64);
-    return std::min(ceil_div(rows, rows_per_block(cols)), 512);
+    const int blocks = ceil_div(rows, rows_per_block(cols));
+    // few values: one block, whose sums are dgain itself, takes less than a second launch
+    if (blocks <= 8 && (long long)rows * cols <= 32768) return 1;
+    return std::min(blocks, 512);
 }
 
 hipError_t launch_norm_backward(int rows, int cols, const Mat& dy, const Mat& sum, const float* gain, const float* rstd,
                                 const Mat& dsum, const Mat& dx, float* dgain, float* partial, hipStream_t s) {
+    const bool direct = norm_partials(rows, cols) == 1;
     if (rows > 0) {
-        const NormBackward a{rows, cols, dy, sum, dsum, dx, gain, rstd, dgain ? partial : nullptr};
+        const NormBackward a{rows, cols, dy, sum, dsum, dx, gain, rstd, !dgain ? nullptr : direct ? dgain : partial};
         hipError_t e;
         if (dy.kind == F32) e = sum.kind == E4M3 ? norm_backward<F32, E4M3>(a, s) : norm_backward<F32, F32>(a, s);
         else e = sum.kind == E4M3 ? norm_backward<BF16, E4M3>(a, s) : norm_backward<BF16, BF16>(a, s);
         if (e != hipSuccess) return e;
     }
-    return dgain ? launch_column_finish(partial, norm_partials(rows, cols), cols, dgain, s) : hipSuccess;
+    return dgain && !direct ? launch_column_finish(partial, norm_partials(rows, cols), cols, dgain, s) : hipSuccess;
 }
 
 hipError_t launch_column_finish(const float* partial, int partials, int cols, float* out, hipStream_t s) {
@@ -427,19 +512,25 @@ hipError_t launch_column_finish(const float* partial, int partials, int cols, fl
     return hipGetLastError();
 }
 
+// Parts of the rows: one as long as a block's walk down all of them costs less than a second launch, then as many as give the
+// chip four blocks a compute unit.
 int slope_partials(int rows, int cols) {
     if (rows == 0) return 0;
-    const int strips = ceil_div(cols, kStripChunks * kChunk);
-    return std::max(1, std::min(ceil_div(rows, 4 * kStripRows), std::max(1, 2048 / strips)));
+    const int strips = ceil_div(cols, kWideStrip * kChunk), step = kThreads / kWideStrip * kSlopeSteps;
+    if (rows <= 256) return 1;
+    return std::max(1, std::min(ceil_div(rows, step), std::max(1, 1024 / strips)));
 }
 
-hipError_t launch_slope(int rows, int cols, const Mat& dy, const Mat& z, int act, const Mat& dz, float* partial,
+hipError_t launch_slope(int rows, int cols, const Mat& dy, const Mat& z, int act, const Mat& dz, float* db, float* partial,
                         hipStream_t s) {
-    if (rows == 0) return hipSuccess;
-    const Slope a{rows, cols, act, dy, z, dz, partial};
     const int parts = slope_partials(rows, cols);
-    if (dy.kind == F32) return act != NONE && z.kind == E4M3 ? slopes<F32, E4M3>(a, parts, s) : slopes<F32, F32>(a, parts, s);
-    return act != NONE && z.kind == E4M3 ? slopes<BF16, E4M3>(a, parts, s) : slopes<BF16, BF16>(a, parts, s);
+    hipError_t e = hipSuccess;
+    if (rows > 0) {
+        const Slope a{rows, cols, act, dy, z, dz, !db ? nullptr : parts == 1 ? db : partial};
+        if (dy.kind == F32) e = act != NONE && z.kind == E4M3 ? slopes<F32, E4M3>(a, parts, s) : slopes<F32, F32>(a, parts, s);
+        else e = act != NONE && z.kind == E4M3 ? slopes<BF16, E4M3>(a, parts, s) : slopes<BF16, BF16>(a, parts, s);
+    }
+    return e == hipSuccess && db && parts != 1 ? launch_column_finish(partial, parts, cols, db, s) : e;
 }
 
 }  // namespace ops

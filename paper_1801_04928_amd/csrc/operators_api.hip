@@ -239,22 +239,17 @@ lf_status lf_linear_backward(int rows, int outputs, int inputs, const lf_matrix*
     // The gradient before the activation: made once, both products read it.
     const bool products = mdx.p || mdw.p;
     Mat dz = mdy;
-    float* const db_partial = db ? (float*)(scratch + at.db_off) : nullptr;
     if (act != LF_ACT_NONE && products) dz = Mat{scratch + at.dz_off, at.dz_ld, nullptr, 0, mdy.kind};
     const Mat made = act != LF_ACT_NONE && products ? dz : Mat{nullptr, 0, nullptr, 0, 0};
-    if (made.p || db) LF_TRY(done(call, lf::ops::launch_slope(rows, outputs, mdy, mz, (int)act, made, db_partial, s)));
-    if (db)
-        LF_TRY(done(call, lf::ops::launch_column_finish(db_partial, lf::ops::slope_partials(rows, outputs), outputs, db, s)));
+    if (made.p || db)
+        LF_TRY(done(call, lf::ops::launch_slope(rows, outputs, mdy, mz, (int)act, made, db, (float*)(scratch + at.db_off), s)));
     const Mat none{nullptr, 0, nullptr, 0, 0};
     float* const raw = (float*)(scratch + at.raw_off);
-    if (mdx.p && rows > 0) {
-        const lf::ops::Product g{dz, mw, false, true, rows, inputs, outputs, {nullptr, LF_ACT_NONE, none, none, mdx}, raw};
-        LF_TRY(done(call, lf::ops::launch_product(g, s)));
-    }
-    if (mdw.p) {
-        const lf::ops::Product g{dz, mx, true, true, outputs, inputs, rows, {nullptr, LF_ACT_NONE, none, none, mdw}, raw};
-        LF_TRY(done(call, lf::ops::launch_product(g, s)));
-    }
+    const lf::ops::Product gx{dz, mw, false, true, rows, inputs, outputs, {nullptr, LF_ACT_NONE, none, none, mdx}, raw};
+    const lf::ops::Product gw{dz, mx, true, true, outputs, inputs, rows, {nullptr, LF_ACT_NONE, none, none, mdw}, raw};
+    if (mdx.p && mdw.p && rows > 0) return done(call, lf::ops::launch_both(gx, gw, s));
+    if (mdx.p && rows > 0) return done(call, lf::ops::launch_product(gx, s));
+    if (mdw.p) return done(call, lf::ops::launch_product(gw, s));
     return LF_OK;
 }
 

@@ -34,9 +34,9 @@ hipError_t launch_norm_backward(int rows, int cols, const Mat& dy, const Mat& su
 hipError_t launch_column_finish(const float* partial, int partials, int cols, float* out, hipStream_t s);
 
 // ---- product_kernels.hip -------------------------------------------------------------------------------------------
-// dz = dy act'(z) into dz (may be absent), and its column sums in `partial` ([slope_partials(rows, cols)][cols], may be null)
+// dz = dy act'(z) into dz (may be absent), and db = its column sums (may be null; partial: [slope_partials(rows, cols)][cols])
 int slope_partials(int rows, int cols);
-hipError_t launch_slope(int rows, int cols, const Mat& dy, const Mat& z, int act, const Mat& dz, float* partial,
+hipError_t launch_slope(int rows, int cols, const Mat& dy, const Mat& z, int act, const Mat& dz, float* db, float* partial,
                         hipStream_t s);
 
 // What is done with a finished element C[m][n] of a product: bias, z kept, activation, residual, y.
@@ -56,6 +56,8 @@ struct Product {
 };
 size_t product_scratch_bytes(int M, int N, int K, bool bf16);
 hipError_t launch_product(const Product& g, hipStream_t s);
+// The two products of a backward pass (the same scratch, one after the other if they use it).
+hipError_t launch_both(const Product& dx, const Product& dw, hipStream_t s);
 
 }  // namespace ops
 }  // namespace lf

@@ -111,11 +111,6 @@ def _storage(dtype):
     raise LfError(LF_EINVAL, f"storage type {dtype!r}: f32 and bf16 are supported")
 
 
-def _check(st: int) -> None:
-    if st != LF_OK:
-        raise LfError(st, lf_operator_error())
-
-
 class E4M3Matrix:
     """rows x cols values in 8 bits: `codes` (uint8, [rows][cols rounded up to whole groups of 32], e4m3) and `scales`
     (uint8, one power of two per group: 2^(byte - 127))."""
@@ -145,13 +140,11 @@ class E4M3Matrix:
     def _set(self, codes, scales, cols):
         self.codes, self.scales, self.cols = codes, scales, cols
         self.rows, self.device = codes.shape[0], codes.device
-        # (a stride of a matrix of one row or none says nothing)
+        self.shape, self._gpu = (self.rows, cols), codes.get_device()
+        # (the stride of one row or of none says nothing)
         self._m = lf_matrix(codes.data_ptr(), max(codes.stride(0), codes.shape[1]), scales.data_ptr(),
                             max(scales.stride(0), scales.shape[1]), LF_MATRIX_E4M3)
-
-    @property
-    def shape(self):
-        return (self.rows, self.cols)
+        self._x = lf_matrix()
 
     def first(self, rows: int) -> "E4M3Matrix":
         """The first rows (no copy)."""
@@ -159,55 +152,67 @@ class E4M3Matrix:
 
     def save(self, x) -> "E4M3Matrix":
         """Keep x ([rows][cols], f32 or bf16)."""
-        _check(lf_checkpoint_save(self.rows, self.cols, _matrix("x", x, self.rows, self.cols, self.device), self._m,
-                                  _stream(self.device)))
-        return self
+        st = _lib().lf_checkpoint_save(self.rows, self.cols, _matrix("x", x, self.shape, self._gpu, self._x), self._m,
+                                       _stream(self._gpu))
+        return self if st == LF_OK else _fail(st)
 
     def load(self, out=None, dtype="bf16"):
         """The values, in `out` or a new tensor of the type."""
         if out is None:
-            out = _torch().empty(self.rows, self.cols, dtype=_storage(dtype)[0], device=self.device)
-        _check(lf_checkpoint_load(self.rows, self.cols, self._m, _matrix("out", out, self.rows, self.cols, self.device),
-                                  _stream(self.device)))
-        return out
+            out = _torch().empty(self.shape, dtype=_storage(dtype)[0], device=self.device)
+        st = _lib().lf_checkpoint_load(self.rows, self.cols, self._m, _matrix("out", out, self.shape, self._gpu, self._x),
+                                       _stream(self._gpu))
+        return out if st == LF_OK else _fail(st)
 
 
-def _stream(device) -> int:
-    return _torch().cuda.current_stream(device).cuda_stream
+def _fail(st: int):
+    raise LfError(st, lf_operator_error())
+
+
+_raw_stream = None
+
+
+def _stream(gpu: int) -> int:
+    """torch's current stream of a GPU.  (`torch.cuda.current_stream` makes an object for it: a microsecond a call.)"""
+    global _raw_stream
+    if _raw_stream is None:
+        _raw_stream = getattr(_torch()._C, "_cuda_getCurrentRawStream", None) or (
+            lambda i: _torch().cuda.current_stream(i).cuda_stream)
+    return _raw_stream(gpu) if gpu >= 0 else 0
 
 
 _TYPES = None
 
 
-def _matrix(name, x, rows, cols, device):
-    """lf_matrix of a tensor or a matrix in 8 bits, which must be rows x cols on the device; None stays None."""
+def _matrix(name, x, shape, gpu, m):
+    """Fills m with a tensor's address and stride, or gives that of a matrix in 8 bits: x must have the shape and lie on the
+    GPU.  None stays None."""
     global _TYPES
     if x is None:
         return None
-    if isinstance(x, E4M3Matrix):
-        if x.rows != rows or x.cols != cols or x.device != device:
-            raise LfError(LF_EINVAL, f"{name}: {rows} x {cols} on {device} is needed, got {x.rows} x {x.cols} on {x.device}")
+    if type(x) is E4M3Matrix:
+        if x.shape != shape or x._gpu != gpu:
+            raise LfError(LF_EINVAL, f"{name}: {shape[0]} x {shape[1]} on GPU {gpu} is needed, got {x.shape} on {x.device}")
         return x._m
     if _TYPES is None:
         t = _torch()
         _TYPES = {t.float32: LF_MATRIX_F32, t.bfloat16: LF_MATRIX_BF16}
     kind = _TYPES.get(x.dtype)
-    if kind is None or x.shape != (rows, cols) or x.device != device:
-        raise LfError(LF_EINVAL, f"{name}: {rows} x {cols}, f32 or bf16, on {device} is needed, got {list(x.shape)}, "
-                                 f"{x.dtype}, on {x.device}")
+    if kind is None or x.shape != shape or x.get_device() != gpu:
+        raise LfError(LF_EINVAL, f"{name}: {shape[0]} x {shape[1]}, f32 or bf16, on GPU {gpu} is needed, got "
+                                 f"{list(x.shape)}, {x.dtype}, on {x.device}")
     ld, inner = x.stride()
-    if rows <= 1:
-        ld = max(ld, cols)          # a stride of one row says nothing
-    if inner != 1 and cols > 1:
+    if inner != 1 and shape[1] > 1:
         raise LfError(LF_EINVAL, f"{name}: rows have to be contiguous, strides are {x.stride()}")
-    return lf_matrix(x.data_ptr(), ld, None, 0, kind)
+    m.data, m.ld, m.type = x.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1]), kind      # (one row's stride says nothing)
+    return m
 
 
-def _vector(name, x, n, device) -> int:
+def _vector(name, x, n, gpu) -> int:
     if x is None:
         return 0
-    if x.dtype != _torch().float32 or x.shape != (n,) or x.device != device or (n > 1 and x.stride(0) != 1):
-        raise LfError(LF_EINVAL, f"{name}: {n} contiguous f32 on {device} are needed, got {list(x.shape)}, {x.dtype}, on "
+    if x.dtype != _torch().float32 or x.shape != (n,) or x.get_device() != gpu or (n > 1 and x.stride(0) != 1):
+        raise LfError(LF_EINVAL, f"{name}: {n} contiguous f32 on GPU {gpu} are needed, got {list(x.shape)}, {x.dtype}, on "
                                  f"{x.device}")
     return x.data_ptr()
 
@@ -220,39 +225,43 @@ class _Operator:
         if passes not in ("forward", "backward", "both"):
             raise LfError(LF_EINVAL, f"passes = {passes!r}: forward, backward or both")
         self.rows, self.device = rows, t.device(device)
-        if self.device.index is None:
-            self.device = t.device(self.device.type, 0)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = t.device("cuda", t.cuda.current_device())
+        self._gpu = -1 if self.device.type == "cpu" else self.device.index
         self.dtype, _, self._dt = _storage(dtype)
         self._forward, self._backward = passes != "backward", passes != "forward"
+        self._in = [lf_matrix() for _ in range(4)]          # of a call's inputs
+        self._whole = {}                                   # lf_matrix of an output of all rows
 
     def _new(self, name, rows, cols, kind):
-        """A matrix of the storage type or, "e4m3", in 8 bits; None for "none"; a matrix of the caller's is taken as it is."""
-        if isinstance(kind, (_torch().Tensor, E4M3Matrix)):
-            _matrix(name, kind, rows, cols, self.device)
-            return kind
+        """An output: a matrix of the storage type or, "e4m3", in 8 bits; None for "none"; a matrix of the caller's is taken as it is."""
         if isinstance(kind, str) and kind == "none":
             return None
         if isinstance(kind, str) and kind == "e4m3":
-            return E4M3Matrix(rows, cols, self.device)
-        return _torch().empty((rows, cols), dtype=_storage(kind)[0], device=self.device)
+            kind = E4M3Matrix(rows, cols, self.device)
+        elif not isinstance(kind, (_torch().Tensor, E4M3Matrix)):
+            kind = _torch().empty((rows, cols), dtype=_storage(kind)[0], device=self.device)
+        self._whole[name] = _matrix(name, kind, (rows, cols), self._gpu, lf_matrix())
+        return kind
+
+    def _some(self, name, whole, n):
+        """(the first n rows of an output, their lf_matrix)"""
+        if n == self.rows or whole is None:
+            return whole, self._whole.get(name)
+        part = whole.first(n) if isinstance(whole, E4M3Matrix) else whole[:n]
+        return part, _matrix(name, part, (n, whole.shape[1]), self._gpu, lf_matrix())
 
     def _scratch(self, nbytes):
         return _torch().empty(nbytes, dtype=_torch().uint8, device=self.device)
 
-    def _need(self, have, what):
+    def _begin(self, x, have, what):
+        """Rows of a call's input."""
+        n = x.shape[0]
+        if n > self.rows:
+            raise LfError(LF_EINVAL, f"{n} rows, the object was made for {self.rows}")
         if not have:
             raise LfError(LF_EINVAL, f"this object was made without its {what} pass")
-
-    def _count(self, x):
-        rows = x.shape[0]
-        if rows > self.rows:
-            raise LfError(LF_EINVAL, f"{rows} rows, the object was made for {self.rows}")
-        return rows
-
-    def _first(self, x, rows):
-        if x is None or rows == self.rows:
-            return x
-        return x.first(rows) if isinstance(x, E4M3Matrix) else x[:rows]
+        return n
 
 
 class RmsNorm(_Operator):
@@ -277,29 +286,32 @@ class RmsNorm(_Operator):
         if self._backward:
             self._dx = self._new("dx", rows, cols, self.dtype if dx is None else dx)
             self.dgain = t.empty(cols, **f32)
-            self._workspace = self._scratch(lf_norm_workspace_bytes(rows, cols))
+            self.workspace_bytes = lf_norm_workspace_bytes(rows, cols)
+            self._workspace = self._scratch(self.workspace_bytes)
 
     def forward(self, x, branch=None):
-        self._need(self._forward, "forward")
-        n, c, dev = self._count(x), self.cols, self.device
-        self.sum, self.y, self.rstd = (self._first(v, n) for v in (self._sum, self._y, self._rstd))
-        _check(lf_norm_forward(n, c, _matrix("x", x, n, c, dev), _matrix("branch", branch, n, c, dev),
-                               _vector("gain", self.gain, c, dev), self.eps, _matrix("sum", self.sum, n, c, dev),
-                               _matrix("y", self.y, n, c, dev), self.rstd.data_ptr(), _stream(dev)))
-        return self.y
+        n, c, gpu, m = self._begin(x, self._forward, "forward"), self.cols, self._gpu, self._in
+        self.sum, msum = self._some("sum", self._sum, n)
+        self.y, my = self._some("out", self._y, n)
+        self.rstd = self._rstd if n == self.rows else self._rstd[:n]
+        shape = (n, c)
+        st = _lib().lf_norm_forward(n, c, _matrix("x", x, shape, gpu, m[0]), _matrix("branch", branch, shape, gpu, m[1]),
+                                    _vector("gain", self.gain, c, gpu), self.eps, msum, my, self._rstd.data_ptr(),
+                                    _stream(gpu))
+        return self.y if st == LF_OK else _fail(st)
 
     def backward(self, dy, dsum=None, stored=None, rstd=None):
         """From dy and the gradient that reaches the sum on other ways.  stored: the sum, if not the last forward pass's,
         in the storage type or in 8 bits; rstd likewise."""
-        self._need(self._backward, "backward")
-        n, c, dev = self._count(dy), self.cols, self.device
+        n, c, gpu, m = self._begin(dy, self._backward, "backward"), self.cols, self._gpu, self._in
         stored, rstd = self.sum if stored is None else stored, self.rstd if rstd is None else rstd
-        self.dx = self._first(self._dx, n)
-        _check(lf_norm_backward(n, c, _matrix("dy", dy, n, c, dev), _matrix("stored", stored, n, c, dev),
-                                _vector("gain", self.gain, c, dev), _vector("rstd", rstd, n, dev),
-                                _matrix("dsum", dsum, n, c, dev), _matrix("dx", self.dx, n, c, dev),
-                                self.dgain.data_ptr(), self._workspace.data_ptr(), self._workspace.numel(), _stream(dev)))
-        return self.dx
+        self.dx, mdx = self._some("dx", self._dx, n)
+        shape = (n, c)
+        st = _lib().lf_norm_backward(n, c, _matrix("dy", dy, shape, gpu, m[0]), _matrix("stored", stored, shape, gpu, m[1]),
+                                     _vector("gain", self.gain, c, gpu), _vector("rstd", rstd, n, gpu),
+                                     _matrix("dsum", dsum, shape, gpu, m[2]), mdx, self.dgain.data_ptr(),
+                                     self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
+        return self.dx if st == LF_OK else _fail(st)
 
 
 class Linear(_Operator):
@@ -317,8 +329,8 @@ class Linear(_Operator):
             raise LfError(LF_EINVAL, f"activation {act!r}: one of {sorted(ACTIVATIONS)}")
         t = _torch()
         self.outputs, self.inputs, self._act = outputs, inputs, ACTIVATIONS[act]
-        self.w = self.b = self.y = self.z = self.dx = self.dw = self.db = None
-        nbytes = 0
+        self.w = self.b = self._mw = self.y = self.z = self.dx = self.dw = self.db = None
+        self._pb = nbytes = 0
         if self._forward:
             self._y = self._new("y", rows, outputs, self.dtype if y is None else y)
             self._z = self._new("z", rows, outputs, z)
@@ -329,32 +341,35 @@ class Linear(_Operator):
             self.db = t.empty(outputs, dtype=t.float32, device=self.device)
             nbytes = max(nbytes, lf_linear_backward_workspace_bytes(rows, outputs, inputs, self._dt))
         self.workspace_bytes = nbytes
+        if workspace is not None and (workspace.dtype != t.uint8 or workspace.get_device() != self._gpu
+                                      or not workspace.is_contiguous() or workspace.numel() < nbytes):
+            raise LfError(LF_EINVAL, f"workspace: {nbytes} contiguous uint8 on GPU {self._gpu} are needed")
         self._workspace = self._scratch(nbytes) if workspace is None else workspace
 
     def set_params(self, w, b=None) -> None:
-        """w: [outputs][inputs] of the storage type; b: [outputs] f32 or None.  Kept by reference."""
-        _matrix("w", w, self.outputs, self.inputs, self.device)
-        _vector("b", b, self.outputs, self.device)
-        self.w, self.b = w, b
+        """Register w ([outputs][inputs], storage type) and b ([outputs] f32, or None).  They are kept by reference: the
+        data may change between passes."""
+        if w.dtype != self.dtype:
+            raise LfError(LF_EINVAL, f"w: {self.dtype} is needed, got {w.dtype}")
+        m = _matrix("w", w, (self.outputs, self.inputs), self._gpu, lf_matrix())
+        self._pb = _vector("b", b, self.outputs, self._gpu)
+        self.w, self.b, self._mw = w, b, m
 
     def forward(self, x, residual=None):
-        self._need(self._forward, "forward")
-        n, o, i, dev = self._count(x), self.outputs, self.inputs, self.device
-        self.y, self.z = self._first(self._y, n), self._first(self._z, n)
-        _check(lf_linear_forward(n, o, i, _matrix("x", x, n, i, dev), _matrix("w", self.w, o, i, dev),
-                                 _vector("b", self.b, o, dev), self._act, _matrix("residual", residual, n, o, dev),
-                                 _matrix("y", self.y, n, o, dev), _matrix("z", self.z, n, o, dev),
-                                 self._workspace.data_ptr(), self._workspace.numel(), _stream(dev)))
-        return self.y
+        n, o, i, gpu, m = self._begin(x, self._forward, "forward"), self.outputs, self.inputs, self._gpu, self._in
+        self.y, my = self._some("y", self._y, n)
+        self.z, mz = self._some("z", self._z, n)
+        st = _lib().lf_linear_forward(n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._mw, self._pb, self._act,
+                                      _matrix("residual", residual, (n, o), gpu, m[1]), my, mz,
+                                      self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
+        return self.y if st == LF_OK else _fail(st)
 
     def backward(self, dy, x, z=None):
         """From dy, the input of the forward pass, and z if it is not the last forward pass's."""
-        self._need(self._backward, "backward")
-        n, o, i, dev = self._count(dy), self.outputs, self.inputs, self.device
-        z = self.z if z is None else z
-        self.dx = self._first(self._dx, n)
-        _check(lf_linear_backward(n, o, i, _matrix("dy", dy, n, o, dev), _matrix("z", z, n, o, dev), self._act,
-                                  _matrix("x", x, n, i, dev), _matrix("w", self.w, o, i, dev),
-                                  _matrix("dx", self.dx, n, i, dev), _matrix("dw", self.dw, o, i, dev),
-                                  self.db.data_ptr(), self._workspace.data_ptr(), self._workspace.numel(), _stream(dev)))
-        return self.dx
+        n, o, i, gpu, m = self._begin(dy, self._backward, "backward"), self.outputs, self.inputs, self._gpu, self._in
+        self.dx, mdx = self._some("dx", self._dx, n)
+        st = _lib().lf_linear_backward(n, o, i, _matrix("dy", dy, (n, o), gpu, m[0]),
+                                       _matrix("z", self.z if z is None else z, (n, o), gpu, m[1]), self._act,
+                                       _matrix("x", x, (n, i), gpu, m[2]), self._mw, mdx, self._whole["dw"],
+                                       self.db.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
+        return self.dx if st == LF_OK else _fail(st)

@@ -173,16 +173,31 @@ def test_errors_are_the_threads_own():
 
 def test_objects_check_their_tensors():
     import torch
-    x = torch.zeros(4, 40)
+    x, e = torch.zeros(4, 40), P.E4M3Matrix(4, 40, device="cpu")
     with pytest.raises(P.LfError, match="x: 4 x 40"):
-        ops._matrix("x", x.double(), 4, 40, x.device)
-    with pytest.raises(P.LfError, match="x: 5 x 40"):
-        ops._matrix("x", x, 5, 40, x.device)
+        e.save(x.double())
+    with pytest.raises(P.LfError, match="x: 4 x 40"):
+        e.save(torch.zeros(5, 40))
+    with pytest.raises(P.LfError, match="x: 4 x 40"):
+        e.save(torch.zeros(160))
     with pytest.raises(P.LfError, match="contiguous"):
-        ops._matrix("x", torch.zeros(40, 4).t(), 4, 40, x.device)
+        e.save(torch.zeros(40, 4).t())
+    with pytest.raises(P.LfError, match="x: 4 x 40"):
+        P.RmsNorm(4, 40, "f32", device="cpu").forward(P.E4M3Matrix(4, 41, device="cpu"))
     with pytest.raises(P.LfError, match="gain"):
-        ops._vector("gain", torch.zeros(80)[::2], 40, x.device)
-    m = ops._matrix("x", torch.zeros(4, 64)[1:2, 1:41], 1, 40, x.device)
+        n = P.RmsNorm(4, 40, "f32", device="cpu")
+        n.gain = torch.zeros(80)[::2]
+        n.forward(x)
+    p = P.Linear(4, 8, 40, "f32", device="cpu")
+    with pytest.raises(P.LfError, match="w: torch.float32"):
+        p.set_params(torch.zeros(8, 40, dtype=torch.bfloat16))
+    with pytest.raises(P.LfError, match="b: 8"):
+        p.set_params(torch.zeros(8, 40), torch.zeros(40))
+    with pytest.raises(P.LfError, match="w is NULL"):
+        p.forward(x)
+    with pytest.raises(P.LfError, match="workspace"):
+        P.Linear(4, 8, 40, "f32", workspace=torch.zeros(8, dtype=torch.uint8), device="cpu")
+    m = ops._matrix("x", torch.zeros(4, 64)[1:2, 1:41], (1, 40), -1, P.lf_matrix())
     assert m.ld >= 40 and m.type == F
     with pytest.raises(P.LfError, match="codes"):
         P.E4M3Matrix.of(torch.zeros(4, 40, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.uint8), 40)
