@@ -129,6 +129,11 @@ __device__ __forceinline__ void shift_down(v4u& a, int s) {                 // e
     b = (s & 1) ? h : b;
     a = s < 8 ? b : v4u{0u, 0u, 0u, 0u};
 }
+__device__ __forceinline__ void shift_down(v4f& a, int s) {                 // four of 32 bits
+    v4f b = (s & 2) ? v4f{a[2], a[3], 0.0f, 0.0f} : a;
+    b = (s & 1) ? v4f{b[1], b[2], b[3], 0.0f} : b;
+    a = s < 4 ? b : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+}
 __device__ __forceinline__ void shift_down(v4f (&a)[2], int s) {            // eight of 32 bits
     const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
     if (s & 4) { a[0] = a[1]; a[1] = zero; }

@@ -8,7 +8,6 @@
 #include "chunks.h"
 
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 namespace lf {
@@ -31,7 +30,7 @@ struct Args {
 
 // Elements of a piece on their way from memory to LDS.
 template <int KIND, int N> struct Raw;
-template <> struct Raw<F32, 8> { v4f a[2]; };
+template <> struct Raw<F32, 4> { v4f a; };
 template <> struct Raw<BF16, 8> { v4u a; };
 template <> struct Raw<E4M3, 8> { v2u a; int byte; };
 template <> struct Raw<E4M3, 16> { v4u a; int byte; };
@@ -43,15 +42,16 @@ template <> struct Raw<E4M3, 16> { v4u a; int byte; };
 // as far ahead as makes it whole and its elements moved down.  That needs rows of at least eight elements; narrower
 // operands are loaded element by element (NARROW).
 //
-// LDS of a tile contiguous along q: [i][q], rows of eight 16-byte pieces, piece p of row i at place p ^ (i & 7): the rows that a
-// matrix operand takes its pieces from then lie in different banks.  Contiguous along i: [q][i]; bf16 is read there by
-// transposing loads, eight rows of 64 bytes at a time (q, q+1, q+2, q+3 and eight further), whose 64-byte segments
-// change places the same way.
+// LDS of a tile contiguous along q: [i][q], rows of eight 16-byte pieces, piece p of row i at place p ^ (i / 2 % 8): the pieces of
+// 16 rows, which LDS serves at once, then lie in different ones of its 64 banks (of rows 128 bytes long two share them).
+// Contiguous along i: [q][i]; bf16 is read there by transposing loads, eight rows of 64 bytes at a time (q, q+1, q+2, q+3 and
+// eight further), whose 64-byte segments change places the same way; of fp32 the two halves of a wave read rows four
+// apart, whose 128-byte segments change places.
 template <class C, int KIND, bool ALONG, int I, int THREADS, bool NARROW>
 struct Tile {
     static constexpr int BK = kRowBytes / (int)sizeof(C);
     static constexpr int kElems = I * BK;
-    static constexpr int kPiece = KIND == E4M3 && sizeof(C) == 2 ? 16 : 8;
+    static constexpr int kPiece = KIND == E4M3 ? (sizeof(C) == 2 ? 16 : 8) : 16 / (int)sizeof(C);
     static constexpr int kPieces = I * BK / kPiece / THREADS;
     static constexpr int kElemBytes = KIND == F32 ? 4 : KIND == BF16 ? 2 : 1;
     static_assert(kPieces * THREADS * kPiece == I * BK, "whole pieces for every thread");
@@ -67,24 +67,25 @@ struct Tile {
     // Elements of a row that exist in memory: 8 bits come in whole groups.
     static __device__ __forceinline__ int in_memory(int n) { return KIND == E4M3 ? whole_groups(n) : n; }
 
-    // What stays the same from k-tile to k-tile: of every piece, its row's offset in the tile (contiguous along q) or its column's
-    // (along i), and the same for its scale.
+    // What stays the same from k-tile to k-tile: the offset of every piece in its tile, and of its scale; contiguous along i also
+    // that of its column alone, for rows past the contraction's end.
     unsigned at[kPieces], scale_at[KIND == E4M3 ? kPieces : 1];
     __device__ __forceinline__ void begin(const Mat& m, int t, int i0, int I_all) {
+        const unsigned ld = (unsigned)m.ld * kElemBytes, scale_ld = (unsigned)m.scale_ld;
 #pragma unroll
         for (int u = 0; u < kPieces; ++u) {
             int i, q;
             place(t, u, i, q);
-            const int row = min(i, I_all - 1 - i0), col = min(i0 + i, in_memory(I_all) - kPiece);
-            at[u] = ALONG ? (unsigned)col * kElemBytes : (unsigned)row * (unsigned)m.ld * kElemBytes;
-            if constexpr (KIND == E4M3) scale_at[u] = ALONG ? (unsigned)(col / kGroup) : (unsigned)row * (unsigned)m.scale_ld;
+            const unsigned row = min(i, I_all - 1 - i0);
+            at[u] = ALONG ? column(i0, i, I_all) * kElemBytes + (unsigned)q * ld : row * ld;
+            if constexpr (KIND == E4M3) scale_at[u] = ALONG ? column(i0, i, I_all) / kGroup + (unsigned)q * scale_ld : row * scale_ld;
         }
     }
-    // I_all: rows of the operand; q_end: where this workgroup's part of the contraction ends.  live: all ones, or zero past its last
-    // tile (anything may be loaded then, nothing looks at it).
-    __device__ __forceinline__ void load(const Mat& m, int t, int i0, int I_all, int q0, int q_end, unsigned live) {
+    static __device__ __forceinline__ unsigned column(int i0, int i, int I_all) { return min(i0 + i, in_memory(I_all) - kPiece); }
+    // I_all: rows of the operand; q_end: where this workgroup's part of the contraction ends.
+    __device__ __forceinline__ void load(const Mat& m, int t, int i0, int I_all, int q0, int q_end) {
         if constexpr (NARROW) {
-            if (live) load_elements(m, t, i0, I_all, q0, q_end);
+            load_elements(m, t, i0, I_all, q0, q_end);
             return;
         }
         const int q_first = min(q0, q_end - 1);
@@ -95,18 +96,19 @@ struct Tile {
         for (int u = 0; u < kPieces; ++u) {
             int i, q;
             place(t, u, i, q);
-            const unsigned row = ALONG ? min(q, q_end - 1 - q_first) : 0;
-            const unsigned col = ALONG ? 0 : min(q0 + q, in_memory(q_end) - kPiece);
-            const unsigned off = (at[u] + (ALONG ? row * ld : col * kElemBytes)) & live;
+            // past the contraction's end: the tile's first row, or the row's last piece
+            const bool there = q_first + q < q_end;
+            const unsigned col = ALONG ? column(i0, i, I_all) : min(q0 + q, in_memory(q_end) - kPiece);
+            const unsigned off = !ALONG ? at[u] + col * kElemBytes : there ? at[u] : col * kElemBytes;
             if constexpr (KIND == F32) {
-                r[u].a[0] = *as_global<const any_v4f>(base + off);
-                r[u].a[1] = *as_global<const any_v4f>(base + off + 16);
+                r[u].a = *as_global<const any_v4f>(base + off);
             } else if constexpr (KIND == BF16) {
                 r[u].a = __builtin_bit_cast(v4u, *as_global<const any_v8bf>(base + off));
             } else {
                 if constexpr (kPiece == 16) r[u].a = *as_global<const v4u>(base + off);
                 else r[u].a = *as_global<const v2u>(base + off);
-                r[u].byte = *as_global<const uint8_t>(scales + ((scale_at[u] + (ALONG ? row * scale_ld : col / kGroup)) & live));
+                r[u].byte = *as_global<const uint8_t>(
+                    scales + (!ALONG ? scale_at[u] + col / kGroup : there ? scale_at[u] : col / kGroup));
             }
         }
     }
@@ -126,18 +128,12 @@ struct Tile {
                     r[u].byte = *as_global<const uint8_t>(m.scales + row * m.scale_ld + col / kGroup);
                 }
             } else {
-                float v[8];
                 typedef typename Stored<KIND>::type T;
-                load_values((const T*)m.p + row * m.ld + col, n, v);
-                if constexpr (KIND == F32) {
-                    r[u].a[0] = v4f{v[0], v[1], v[2], v[3]};
-                    r[u].a[1] = v4f{v[4], v[5], v[6], v[7]};
-                } else {
-                    v8bf b;
+                const T* p = (const T*)m.p + row * m.ld + col;
+                T v[kPiece];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) b[e] = (__bf16)v[e];
-                    r[u].a = __builtin_bit_cast(v4u, b);
-                }
+                for (int e = 0; e < kPiece; ++e) v[e] = e < n ? *as_global<const T>(p + e) : (T)0.0f;
+                __builtin_memcpy(&r[u].a, v, 16);
             }
         }
     }
@@ -152,7 +148,7 @@ struct Tile {
                 keep_codes(r[u].a, ALONG ? (dead ? 0 : kPiece) : q_end - q0 - q);
             } else if constexpr (!NARROW) {
                 const int s = ALONG ? max(0, i0 + i - (I_all - kPiece)) : max(0, q0 + q - (q_end - kPiece));
-                shift_down(r[u].a, dead ? 8 : s);
+                shift_down(r[u].a, dead ? kPiece : s);
             }
         }
     }
@@ -162,7 +158,7 @@ struct Tile {
 
     // Where 16-byte pieces go.
     static __device__ __forceinline__ int at_along_q(int i, int piece) {
-        return i * BK + ((piece ^ (i & 7)) * (16 / (int)sizeof(C)));
+        return i * BK + ((piece ^ ((i >> 1) & 7)) * (16 / (int)sizeof(C)));
     }
     static __device__ __forceinline__ int at_along_i(int q, int i) {
         if constexpr (sizeof(C) == 2) {
@@ -170,7 +166,7 @@ struct Tile {
             const int turn = ((q & 3) | ((q >> 1) & 4)) & (kSegments < 8 ? kSegments - 1 : 7);
             return q * I + (((i >> 5) ^ turn) << 5) + (i & 31);
         } else {
-            return q * I + i;
+            return q * I + (i ^ ((q & 4) << 3));
         }
     }
     __device__ __forceinline__ void store(C* s, int t) const {
@@ -178,8 +174,8 @@ struct Tile {
         for (int u = 0; u < kPieces; ++u) {
             int i, q;
             place(t, u, i, q);
-            if constexpr (KIND == BF16) {
-                *reinterpret_cast<v4u*>(s + (ALONG ? at_along_i(q, i) : at_along_q(i, q / 8))) = r[u].a;
+            if constexpr (KIND != E4M3) {
+                *reinterpret_cast<decltype(r[u].a)*>(s + (ALONG ? at_along_i(q, i) : at_along_q(i, q / kPiece))) = r[u].a;
             } else if constexpr (sizeof(C) == 2) {
                 const float scale = scale_value(r[u].byte);
 #pragma unroll
@@ -195,15 +191,10 @@ struct Tile {
                 }
             } else {
                 v4f a, b;
-                if constexpr (KIND == F32) {
-                    a = r[u].a[0];
-                    b = r[u].a[1];
-                } else {
-                    float v[8];
-                    eight_values(r[u].a, scale_value(r[u].byte), v);
-                    a = v4f{v[0], v[1], v[2], v[3]};
-                    b = v4f{v[4], v[5], v[6], v[7]};
-                }
+                float v[8];
+                eight_values(r[u].a, scale_value(r[u].byte), v);
+                a = v4f{v[0], v[1], v[2], v[3]};
+                b = v4f{v[4], v[5], v[6], v[7]};
                 if constexpr (ALONG) {
                     *reinterpret_cast<v4f*>(s + at_along_i(q, i)) = a;
                     *reinterpret_cast<v4f*>(s + at_along_i(q, i + 4)) = b;
@@ -218,6 +209,9 @@ struct Tile {
     // Operand of one 32-row tile for step `step` of BK: bf16, 16 q a step: lane holds q = 16 step + 8 (lane / 32) .. +7 of row
     // lane % 32.  fp32, 8 q a step: q = 8 step + 4 (lane / 32) .. +3, one matrix instruction for each.
     typedef typename std::conditional<sizeof(C) == 2, v8bf, v4f>::type Operand;
+    // instructions that a tile takes: requests, stores to LDS, and loads of one operand from there
+    static constexpr int kRequests = kPieces * (KIND == E4M3 ? 2 : 1);
+    static constexpr int kStores = kElems * (int)sizeof(C) / 16 / THREADS, kReads = ALONG ? 2 : 1;
     static constexpr int kSteps = BK / (sizeof(C) == 2 ? 16 : 8);
     static __device__ __forceinline__ Operand operand(const C* s, int i_base, int step) {
         const int lane = threadIdx.x & 63, r32 = lane & 31, half = lane >> 5;
@@ -251,10 +245,6 @@ struct Tile {
 };
 
 // ---- what happens to finished sums -------------------------------------------------------------------------------------
-__device__ __forceinline__ void load_any(const Mat& m, long long row, int col, int n, float (&v)[8]) {
-    if (m.kind == F32) load_chunk<F32>(m, row, col, n, v);
-    else load_chunk<BF16>(m, row, col, n, v);
-}
 __device__ __forceinline__ void store_any(const Mat& m, long long row, int col, int n, const float (&v)[8], bool live) {
     if (m.kind == E4M3) store_chunk<E4M3>(m, row, col, n, v, live);
     else if (m.kind == F32) store_chunk<F32>(m, row, col, n, v, live);
@@ -265,18 +255,23 @@ __device__ __forceinline__ void activate_all(float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = activate(ACT, v[i]);
 }
+// The residual has the storage type, which is C's.  Zeros if there is none, or no such row.
+template <class C>
+__device__ __forceinline__ void load_residual(const Finish& f, int M, int m, int n, int there, float (&r)[8]) {
+    if (f.residual.p && m < M) {
+        load_values((const C*)f.residual.p + m * f.residual.ld + n, there, r);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = 0.0f;
+    }
+}
 // Eight columns of row m from n on (n a multiple of 8; the four lanes of a quad hold the four chunks of a group of 32).
-__device__ __forceinline__ void finish_chunk(const Finish& f, int M, int N, int m, int n, float (&v)[8]) {
+__device__ __forceinline__ void finish_chunk(const Finish& f, int M, int N, int m, int n, float (&v)[8], const float (&bias)[8],
+                                             const float (&residual)[8]) {
     const int there = m < M ? min(N - n, kChunk) : 0;
     const bool live = m < M && n < whole_groups(N);
-    if (f.bias && there > 0) {
-        float b[8];
-        load_values(f.bias + n, there, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += b[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < there ? v[i] : 0.0f;
+    for (int i = 0; i < 8; ++i) v[i] = i < there ? v[i] + bias[i] : 0.0f;
     if (f.z.p) store_any(f.z, m, n, there, v, live);
     switch (f.act) {                        // (the branch is outside the loop over the eight values)
         case SIGMOID: activate_all<SIGMOID>(v); break;
@@ -285,40 +280,53 @@ __device__ __forceinline__ void finish_chunk(const Finish& f, int M, int N, int 
         case GELU: activate_all<GELU>(v); break;
         default: break;
     }
-    if (f.residual.p) {
-        float r[8];
-        load_any(f.residual, m, n, there, r);
+    // (past the row's end zeros: sigmoid(0) is not 0, and a group's scale looks at all of its values)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += r[i];
-    }
-    if (f.y.kind == E4M3) {      // sigmoid(0) is not 0
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < there ? v[i] : 0.0f;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = i < there ? v[i] + residual[i] : 0.0f;
     store_any(f.y, m, n, there, v, live);
 }
 
+// The order in which a step's instructions are issued, as scheduling groups (0x008 matrix instruction, 0x020 request, 0x100
+// LDS read, 0x200 LDS write): after every matrix instruction its share of the next step's reads, all of them in the step's
+// first half, of the writes to LDS and of the requests into the registers these have left.  The compiler by itself puts all
+// writes and requests before the first matrix instruction, and those stand still meanwhile.
+template <int MASK, int N> __device__ __forceinline__ void issue() {
+    if constexpr (N > 0) __builtin_amdgcn_sched_group_barrier(MASK, N, 0);
+}
+template <int M, int READS, int WRITES, int REQUESTS, int I = 0>
+__device__ __forceinline__ void interleave() {
+    if constexpr (I < M) {
+        constexpr int window = M >= 8 ? M : M > 1 ? M / 2 : 1, a = I < window ? I : window, b = I < window ? I + 1 : window;
+        issue<0x008, 1>();
+        issue<0x100, READS * b / window - READS * a / window>();
+        issue<0x200, WRITES * (I + 1) / M - WRITES * I / M>();
+        issue<0x020, REQUESTS * (I + 1) / M - REQUESTS * I / M>();
+        interleave<M, READS, WRITES, REQUESTS, I + 1>();
+    }
+}
+
 // ================================================================================================
-// tiles of BM x BN; KS groups of WM x WN waves share a tile's contraction
+// tiles of BM x BN by WM x WN waves
 // ================================================================================================
-// A group walks every KS-th k-tile of its workgroup's part.  D k-tiles of it are under way in registers, one lies in LDS for the
-// multiplications, and one is laid beside it meanwhile: one barrier a k-tile.
+// Of KS groups of WM x WN waves each walks every KS-th k-tile of its workgroup's part.  D k-tiles are under way in registers,
+// one lies in LDS for the multiplications, and one is laid beside it meanwhile.  The two buffers are arrays of their own, so
+// that the compiler knows the writes to one and the reads of the other apart.
 template <class C, int BM, int BN, int KS>
-constexpr int kLdsElems = KS * 2 * (BM + BN) * (kRowBytes / (int)sizeof(C));
+constexpr int kLdsElems = KS * (BM + BN) * (kRowBytes / (int)sizeof(C));
 
 template <class C, int PK, int QK, bool P_ALONG, bool Q_ALONG, int BM, int BN, int WM, int WN, int KS, int D, bool NARROW>
-__device__ __forceinline__ void product_tile(const Args& g, unsigned block, C* lds) {
+__device__ __forceinline__ void product_tile(const Args& g, unsigned block, C* lds0, C* lds1) {
     constexpr int kThreads = 64 * WM * WN;
     typedef Tile<C, PK, P_ALONG, BM, kThreads, NARROW> TP;
     typedef Tile<C, QK, Q_ALONG, BN, kThreads, NARROW> TQ;
     constexpr int BK = TP::BK, MT = BM / WM / 32, NT = BN / WN / 32;
-    constexpr int kBuffer = TP::kElems + TQ::kElems;
-    // rows of the epilogue's staging: with groups all of the tile's, else as many of a wave's own as fit
-    constexpr int kStageLd = KS > 1 ? BN + 4 : NT * 32 + 4;
-    constexpr int kStageRows = KS > 1 ? BM : WM * WN * 32 * kStageLd * 4 <= 2 * kBuffer * (int)sizeof(C) ? 32 : 16;
-    static_assert((KS > 1 ? 1 : WM * WN) * kStageRows * kStageLd * 4 <= 2 * kBuffer * (int)sizeof(C), "the staging fits");
+    static_assert(D == 1 || D == 2, "a k-tile's registers and buffer are known when it is compiled");
+    // the epilogue's staging, half of the waves in either buffer: as many rows of a wave's own as fit
+    constexpr int kStageLd = NT * 32 + 4, kHalf = WM * WN / 2, kFit = kLdsElems<C, BM, BN, KS> * (int)sizeof(C) / (kHalf * kStageLd * 4);
+    constexpr int kStageRows = kFit >= 32 ? 32 : 16;
+    static_assert(kFit >= 16, "the staging fits");
 
-    const int t = threadIdx.x % kThreads, group = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    const int t = threadIdx.x % kThreads, group = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     // Workgroups are dealt to the 8 XCDs in turn: an XCD takes neighbouring tiles (and, of a split product, one split's).
     const int tiles = g.tiles_m * g.tiles_n, total = tiles * g.splits;
@@ -333,13 +341,17 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, C* l
     const int q_end = min(g.K, kt1 * BK);
     const int turns = ceil_div(kt1 - kt0, KS);
 
-    v16f acc[MT][NT];
+    // (two sums of a wave's only 32 x 32 square, taken in turn: a matrix instruction would wait for the one before it)
+    constexpr int kChains = MT * NT == 1 ? 2 : 1;
+    v16f acc[MT][NT][kChains];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+            for (int c = 0; c < kChains; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][c][e] = 0.0f;
 
     TP tp[D];
     TQ tq[D];
@@ -349,182 +361,319 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, C* l
         tp[d].begin(g.P, t, m0, g.M);
         tq[d].begin(g.Q, t, n0, g.N);
     }
+    // (past the last k-tile the last one again, which nothing looks at: no branch around the loads)
     auto request = [&](int d, int turn) {
-        // (an operand of the address, not a branch around the load)
-        const unsigned live = __builtin_amdgcn_readfirstlane(turn < turns ? ~0u : 0u);
-        tp[d].load(g.P, t, m0, g.M, q_of(turn), q_end, live);
-        tq[d].load(g.Q, t, n0, g.N, q_of(turn), q_end, live);
+        const int q0 = q_of(min(turn, turns - 1));
+        tp[d].load(g.P, t, m0, g.M, q0, q_end);
+        tq[d].load(g.Q, t, n0, g.N, q0, q_end);
     };
-    C* const mine = lds + group * 2 * kBuffer;
-    auto lay = [&](int d, int turn) {
+    auto mend = [&](int d, int turn) {
         const int q0 = q_of(turn);
         if (TP::at_end(m0, g.M, q0, q_end)) tp[d].mend(t, m0, g.M, q0, q_end);
         if (TQ::at_end(n0, g.N, q0, q_end)) tq[d].mend(t, n0, g.N, q0, q_end);
-        C* const buffer = mine + (turn & 1) * kBuffer;
+    };
+    auto lay = [&](int d, C* buffer) {
         tp[d].store(buffer, t);
         tq[d].store(buffer + TP::kElems, t);
     };
-    auto multiply = [&](int turn) {
-        const C* const sp = mine + (turn & 1) * kBuffer;
-        const C* const sq = sp + TP::kElems;
+    typename TP::Operand a[2][MT], q[2][NT];
+    auto read = [&](const C* sp, auto step) {
 #pragma unroll
-        for (int step = 0; step < TP::kSteps; ++step) {
-            typename TP::Operand a[MT], q[NT];
+        for (int i = 0; i < MT; ++i) a[step() % 2][i] = TP::operand(sp, wm + 32 * i, step());
 #pragma unroll
-            for (int i = 0; i < MT; ++i) a[i] = TP::operand(sp, wm + 32 * i, step);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) q[j] = TQ::operand(sq, wn + 32 * j, step);
+        for (int j = 0; j < NT; ++j) q[step() % 2][j] = TQ::operand(sp + TP::kElems, wn + 32 * j, step());
+    };
+    auto multiply = [&](auto step) {
+        constexpr int set = step() % 2;
+        if constexpr (sizeof(C) == 2) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    if constexpr (sizeof(C) == 2) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], q[j], acc[i][j], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i][e], q[j][e], acc[i][j], 0, 0, 0);
-                    }
+                    v16f& sum = acc[i][j][step() % kChains];
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[set][i], q[set][j], sum, 0, 0, 0);
                 }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        v16f& sum = acc[i][j][e % kChains];
+                        sum = __builtin_amdgcn_mfma_f32_32x32x2f32(a[set][i][e], q[set][j][e], sum, 0, 0, 0);
+                    }
+        }
+    };
+    C* const buffers[2] = {lds0 + group * (TP::kElems + TQ::kElems), lds1 + group * (TP::kElems + TQ::kElems)};
+    constexpr std::integral_constant<int, 0> s0;
+    constexpr std::integral_constant<int, 1> s1;
+    constexpr std::integral_constant<int, 2> s2;
+    constexpr std::integral_constant<int, 3> s3;
+    static_assert(TP::kSteps == 4, "the steps below");
+    constexpr int kMfmas = MT * NT * (sizeof(C) == 2 ? 1 : 4), kStepReads = MT * TP::kReads + NT * TQ::kReads;
+    constexpr int kWrites = TP::kStores + TQ::kStores, kRequests = TP::kRequests + TQ::kRequests;
+    // Multiplies a k-tile and lays the next one, which goes to the buffer that all waves had read before the last barrier.  EARLY:
+    // the barrier stands before the last step, whose operands are in registers by then, and the next tile's first operands are
+    // read while it is multiplied.  (Of 256 x 256 tiles these registers are not there: they would be spilled.)
+    constexpr bool EARLY = MT * NT <= 4;
+    const auto k_tile = [&](int turn, auto at) {
+        constexpr int d = at(), next = (d + 1) % D;
+        mend(next, turn + 1);
+        lay(next, buffers[(d + 1) & 1]);
+        request(next, turn + 1 + D);
+        if constexpr (!EARLY) {
+            read(buffers[d & 1], s0);
+            issue<0x100, kStepReads>();
+        }
+        read(buffers[d & 1], s1);
+        multiply(s0);
+        read(buffers[d & 1], s2);
+        multiply(s1);
+        read(buffers[d & 1], s3);
+        multiply(s2);
+        if constexpr (!NARROW) {
+            interleave<kMfmas, kStepReads, kWrites / 3, kRequests / 3>();
+            interleave<kMfmas, kStepReads, kWrites * 2 / 3 - kWrites / 3, kRequests * 2 / 3 - kRequests / 3>();
+            interleave<kMfmas, kStepReads, kWrites - kWrites * 2 / 3, kRequests - kRequests * 2 / 3>();
+        }
+        if constexpr (EARLY) {
+            __syncthreads();
+            read(buffers[(d + 1) & 1], s0);
+            multiply(s3);
+            if constexpr (!NARROW) interleave<kMfmas, kStepReads, 0, 0>();
+        } else {
+            multiply(s3);
+            interleave<kMfmas, 0, 0, 0>();
+            __syncthreads();
         }
     };
     if (turns > 0) {
 #pragma unroll
         for (int d = 0; d < D; ++d) request(d, d);
-        lay(0, 0);
+        mend(0, 0);
+        lay(0, buffers[0]);
         request(0, D);
         __syncthreads();
-        for (int turn = 0;; turn += D) {
+        if constexpr (EARLY) read(buffers[0], s0);
+        int turn = 0;
+        // (a way out between the two would cost the sums a second set of registers)
+        for (; turn + 1 < turns; turn += 2) {
+            k_tile(turn, s0);
+            k_tile(turn + 1, s1);
+        }
+        if (turn < turns) {
+            if constexpr (!EARLY) read(buffers[0], s0);
+            read(buffers[0], s1);
+            multiply(s0);
+            read(buffers[0], s2);
+            multiply(s1);
+            read(buffers[0], s3);
+            multiply(s2);
+            multiply(s3);
+        }
+        __syncthreads();          // the buffers become the epilogue's
+    }
+    if constexpr (kChains == 2) acc[0][0][0] += acc[0][0][1];
+    if constexpr (KS > 1) {
+        // the first group adds the others' sums, in their order, and finishes the tile
+        static_assert(KS <= 4 && kThreads * MT * NT * 16 * (KS - 1) * 4 <= 3 * kLdsElems<C, BM, BN, KS> * (int)sizeof(C) / 4, "");
+        v4f* sums = reinterpret_cast<v4f*>(lds0);
+        for (int k = 0; k < KS - 1; ++k) {
 #pragma unroll
-            for (int d = 0; d < D; ++d) {
-                // k-tile turn + d + 1 goes to the buffer that was read before the last barrier
-                lay((d + 1) % D, turn + d + 1);
-                request((d + 1) % D, turn + d + 1 + D);
-                multiply(turn + d);
-                __syncthreads();
-                if (turn + d + 1 == turns) goto multiplied;
+            for (int u = 0; u < 4; ++u) {
+                v4f& at = sums[(k * 4 + u) * kThreads + t];
+                const v16f s = acc[0][0][0];
+                if (group == k + 1) at = v4f{s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]};
             }
         }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const v4f s = sums[(k * 4 + u) * kThreads + t];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[0][0][0][4 * u + e] += s[e];
+            }
+        lds0 += (KS - 1) * kThreads * 16 * (int)(sizeof(float) / sizeof(C));
     }
-multiplied:
 
     // Accumulator element e of lane (r32, half) of tile (i, j) is C[.. 32 i + 8 (e / 4) + 4 half + e % 4][.. 32 j + r32].  Rows turn
     // through LDS, so that a lane holds eight consecutive columns.
     const int r32 = lane & 31, half = lane >> 5;
-    auto finish = [&](int m, int n, float (&v)[8]) {
-        if (g.splits > 1) {
-            if (m < g.M && n < g.N) store_values(g.raw + ((size_t)split * g.M + m) * g.N + n, g.N - n, v);
-        } else {
-            finish_chunk(g.f, g.M, g.N, m, n, v);
-        }
-    };
-    if constexpr (KS > 1) {
-        // every group lays its sums down, all threads add them up
-        float* stage = reinterpret_cast<float*>(mine);
+    // in LDS of the wave's own: nobody waits
+    float* stage = reinterpret_cast<float*>(wave < kHalf ? lds0 : lds1) + wave % kHalf * (kStageRows * kStageLd);
+    constexpr int kAcross = NT * 4, kDown = 64 / kAcross;      // lanes along a row, rows at once
+    constexpr int kElems = kStageRows / 2;                     // accumulator elements that hold these rows
+    const int n = n0 + wn + lane % kAcross * kChunk, n_there = min(max(g.N - n, 0), kChunk);
+    // the column stays the same: its bias is loaded once; a residual is under way while the rows before it are finished
+    float bias[8];
+    if (g.f.bias && g.splits == 1) {
+        load_values(g.f.bias + n, n_there, bias);
+    } else {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int h = 0; h < 16 / kElems; ++h) {
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    stage[(wm + 32 * i + 8 * (e >> 2) + 4 * half + (e & 3)) * kStageLd + wn + 32 * j + r32] = acc[i][j][e];
-        __syncthreads();
-        constexpr int kChunks = BM * BN / kChunk;
-        // (one copy of what follows in the code, here and below: an epilogue unrolled is larger than the instruction cache)
+                for (int e = 0; e < kElems; ++e)
+                    stage[(8 * (e >> 2) + 4 * half + (e & 3)) * kStageLd + 32 * j + r32] = acc[i][j][0][kElems * h + e];
+            __builtin_amdgcn_wave_barrier();
+            // (one copy of what follows in the code: an epilogue unrolled is larger than the instruction cache)
+            const int first = m0 + wm + 32 * i + kStageRows * h;
+            float residual[8];
+            load_residual<C>(g.f, g.M, first + lane / kAcross, n, n_there, residual);
 #pragma unroll 1
-        for (int chunk = threadIdx.x; chunk < kChunks; chunk += kThreads * KS) {
-            const int row = chunk / (BN / kChunk), col = chunk % (BN / kChunk) * kChunk;
-            float v[8] = {};
+            for (int row = lane / kAcross; row < kStageRows; row += kDown) {
+                const int col = lane % kAcross * kChunk, m = first + row;
+                const v4f lo = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col);
+                const v4f hi = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col + 4);
+                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, r[8];
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const float* from = reinterpret_cast<const float*>(lds + k * 2 * kBuffer) + row * kStageLd + col;
-                const v4f lo = *reinterpret_cast<const v4f*>(from), hi = *reinterpret_cast<const v4f*>(from + 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { v[i] += lo[i]; v[4 + i] += hi[i]; }
-            }
-            finish(m0 + row, n0 + col, v);
-        }
-    } else {
-        // in LDS of the wave's own: nobody waits
-        float* stage = reinterpret_cast<float*>(lds) + wave * kStageRows * kStageLd;
-        constexpr int kAcross = NT * 4, kDown = 64 / kAcross;      // lanes along a row, rows at once
-        constexpr int kElems = kStageRows / 2;                     // accumulator elements that hold these rows
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int h = 0; h < 16 / kElems; ++h) {
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int e = 0; e < kElems; ++e)
-                        stage[(8 * (e >> 2) + 4 * half + (e & 3)) * kStageLd + 32 * j + r32] = acc[i][j][kElems * h + e];
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-                for (int row = lane / kAcross; row < kStageRows; row += kDown) {
-                    const int col = lane % kAcross * kChunk;
-                    const v4f lo = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col);
-                    const v4f hi = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col + 4);
-                    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                    finish(m0 + wm + 32 * i + kStageRows * h + row, n0 + wn + col, v);
+                for (int u = 0; u < 8; ++u) r[u] = residual[u];
+                load_residual<C>(g.f, g.M, row + kDown < kStageRows ? m + kDown : g.M, n, n_there, residual);
+                if (g.splits > 1) {
+                    if (m < g.M && n_there > 0) store_values(g.raw + ((size_t)split * g.M + m) * g.N + n, n_there, v);
+                } else {
+                    finish_chunk(g.f, g.M, g.N, m, n, v, bias, r);
                 }
-                __builtin_amdgcn_wave_barrier();
             }
-    }
+            __builtin_amdgcn_wave_barrier();
+        }
 }
 
 template <class C, int PK, int QK, bool P_ALONG, bool Q_ALONG, int BM, int BN, int WM, int WN, int KS, int D, bool NARROW>
 __global__ __launch_bounds__(64 * WM * WN * KS) void k_product(const Args g) {
-    __shared__ __attribute__((aligned(16))) C lds[kLdsElems<C, BM, BN, KS>];
-    product_tile<C, PK, QK, P_ALONG, Q_ALONG, BM, BN, WM, WN, KS, D, NARROW>(g, blockIdx.x, lds);
+    __shared__ __attribute__((aligned(16))) C lds0[kLdsElems<C, BM, BN, KS>];
+    __shared__ __attribute__((aligned(16))) C lds1[kLdsElems<C, BM, BN, KS>];
+    product_tile<C, PK, QK, P_ALONG, Q_ALONG, BM, BN, WM, WN, KS, D, NARROW>(g, blockIdx.x, lds0, lds1);
 }
 
 // Both products of a backward pass in one launch: the first `first` workgroups take dx, the others dw.
 template <class C, int T, int XK, int BM, int BN, int WM, int WN, int KS, int D>
 __global__ __launch_bounds__(64 * WM * WN * KS) void k_both(const Args dx, const Args dw, unsigned first) {
-    __shared__ __attribute__((aligned(16))) C lds[kLdsElems<C, BM, BN, KS>];
-    if (blockIdx.x < first) product_tile<C, T, T, false, true, BM, BN, WM, WN, KS, D, false>(dx, blockIdx.x, lds);
-    else product_tile<C, T, XK, true, true, BM, BN, WM, WN, KS, D, false>(dw, blockIdx.x - first, lds);
+    __shared__ __attribute__((aligned(16))) C lds0[kLdsElems<C, BM, BN, KS>];
+    __shared__ __attribute__((aligned(16))) C lds1[kLdsElems<C, BM, BN, KS>];
+    if (blockIdx.x < first) product_tile<C, T, T, false, true, BM, BN, WM, WN, KS, D, false>(dx, blockIdx.x, lds0, lds1);
+    else product_tile<C, T, XK, true, true, BM, BN, WM, WN, KS, D, false>(dw, blockIdx.x - first, lds0, lds1);
 }
 
 // Sums of the splits' partial sums, in their order, and what follows.
 constexpr int kJoinThreads = 256;
+template <class C>
 __global__ __launch_bounds__(kJoinThreads) void k_join(const float* raw, int splits, int M, int N, int chunks, const Finish f) {
     const long long id = (long long)blockIdx.x * kJoinThreads + threadIdx.x;
     const long long row = id / chunks;
     const int n = (int)(id % chunks) * kChunk;
     const int m = row < M ? (int)row : M;                     // lanes past the end stay with their quads
-    float v[8] = {};
-    if (m < M && n < N) {
+    const int there = m < M ? min(max(N - n, 0), kChunk) : 0;
+    float v[8] = {}, bias[8] = {}, residual[8];
+    if (f.bias) load_values(f.bias + n, there, bias);
+    load_residual<C>(f, M, m, n, there, residual);
+    if (there > 0) {
         for (int p = 0; p < splits; ++p) {
             float u[8];
-            load_values(raw + ((size_t)p * M + m) * N + n, N - n, u);
+            load_values(raw + ((size_t)p * M + m) * N + n, there, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += u[i];
         }
     }
-    finish_chunk(f, M, N, m, n, v);
+    finish_chunk(f, M, N, m, n, v, bias, residual);
+}
+
+// ================================================================================================
+// a few rows
+// ================================================================================================
+// One sample, or up to four: the product is the reading of w.  A wave takes two outputs and walks their rows of w, 512 q a
+// step, with the same q of x; a workgroup's outputs are whole chunks, or whole groups of 32 (WAVES = 16) where the results
+// are kept in 8 bits.  Bound by memory: all of a wave's requests for some thousand q are under way at once.
+constexpr int kFewRows = 4, kFewOutputs = 2;
+template <class C, int XK, int ROWS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_few(const Args g) {
+    constexpr int kStep = 64 * kChunk, kUnroll = ROWS == 1 ? 4 : ROWS == 4 && XK == E4M3 ? 1 : 2, kOutputs = WAVES * kFewOutputs;
+    __shared__ float sums[ROWS][kOutputs];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * kOutputs, n = n0 + wave * kFewOutputs;
+    float sum[ROWS][kFewOutputs] = {};
+    const auto step = [&](int q0, auto unroll, bool whole) {
+        constexpr int U = unroll();
+        float x[U][ROWS][8], w[U][kFewOutputs][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int q = q0 + u * kStep + lane * kChunk, there = whole ? kChunk : min(g.K - q, kChunk);
+#pragma unroll
+            for (int o = 0; o < kFewOutputs; ++o)
+                load_values((const C*)g.Q.p + min(n + o, g.N - 1) * g.Q.ld + q, there, w[u][o]);
+#pragma unroll
+            for (int m = 0; m < ROWS; ++m) load_chunk<XK>(g.P, min(m, g.M - 1), q, there, x[u][m]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int m = 0; m < ROWS; ++m)
+#pragma unroll
+                for (int o = 0; o < kFewOutputs; ++o)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[m][o] = fmaf(x[u][m][e], w[u][o][e], sum[m][o]);
+    };
+    int q0 = 0;
+    for (; q0 + kUnroll * kStep <= g.K; q0 += kUnroll * kStep) step(q0, std::integral_constant<int, kUnroll>(), true);
+    for (; q0 < g.K; q0 += kStep) step(q0, std::integral_constant<int, 1>(), false);
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m)
+#pragma unroll
+        for (int o = 0; o < kFewOutputs; ++o) {
+            const float all = wave_sum(sum[m][o]);
+            if (lane == 0) sums[m][wave * kFewOutputs + o] = all;
+        }
+    __syncthreads();
+    constexpr int kChunks = kOutputs / kChunk;
+    if (threadIdx.x >= ROWS * kChunks) return;
+    const int m = threadIdx.x / kChunks, col = threadIdx.x % kChunks * kChunk, there = min(max(g.N - n0 - col, 0), kChunk);
+    float v[8], bias[8] = {}, residual[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = sums[m][col + i];
+    if (g.f.bias) load_values(g.f.bias + n0 + col, there, bias);
+    load_residual<C>(g.f, g.M, m, n0 + col, there, residual);
+    finish_chunk(g.f, g.M, g.N, m, n0 + col, v, bias, residual);
 }
 
 // ---- which tiles ---------------------------------------------------------------------------------------------------------
-struct Plan { int bm, bn, groups, splits, k_tiles_per_split; };
+struct Plan { int bm, bn, splits, k_tiles_per_split; };
 constexpr int kGroups = 256;             // workgroups that fill the chip
 constexpr int kLeastTiles = 4;           // of the contraction a split has
 
+// The plan that takes the least time by the measurements: us a turn of kGroups workgroups takes for 1024 of the contraction, with 5 us
+// around; splits store their sums and read them again at 5 TB/s, in a launch more.  Measured, us, 64 | 128 | 256, bf16 rows x
+// 4096 x 4096: 256 rows 20 | 23 | 41, 512 31 | 31 | 43, 1024 55 | 41 | 55, 2048 105 | 73 | 83, 4096 205 | 138 | 117; 512 x 8192 x
+// 8192 105 | 72 | 81, 4096 x 8192 x 8192 818 | 509 | 425; 1024 x 2048 x 2048 17 | 25 | 37.
 Plan plan_of(int M, int N, int K, bool bf16) {
     const int k_tiles = ceil_div(K, bf16 ? 64 : 32);
-    Plan p{64, 64, 1, 1, k_tiles};
-    const auto tiles_of = [&](int b) { return (long long)ceil_div(M, b) * ceil_div(N, b); };
-    if (const char* e = getenv("PLAN")) { p.bm = p.bn = atoi(e); if (p.bm > 256) { p.bm = p.bn = 64; p.groups = 4; } }
-    else if (bf16 && tiles_of(256) >= 200) p.bm = p.bn = 256;
-    else if (tiles_of(128) >= 128) p.bm = p.bn = 128;
-    const long long tiles = tiles_of(p.bm);
-    int want = (int)std::max<long long>(1, std::min<long long>(kGroups / tiles, k_tiles / kLeastTiles));
-    if (const char* e = getenv("SPLIT")) want = std::max(1, std::min(atoi(e), want));
-    if (want > 1) {
-        p.k_tiles_per_split = ceil_div(k_tiles, want);
-        p.splits = ceil_div(k_tiles, p.k_tiles_per_split);
+    const struct { int tile; double us; } kinds[] = {{64, bf16 ? 3.1 : 16.0}, {128, 8.4}, {256, 27.0}};
+    Plan best{64, 64, 1, k_tiles};
+    double least = 1e300;
+    for (const auto& kind : kinds) {
+        if (!bf16 && kind.tile > 64) break;
+        const long long tiles = (long long)ceil_div(M, kind.tile) * ceil_div(N, kind.tile);
+        const int most = (int)std::max<long long>(1, std::min<long long>(kGroups / tiles, k_tiles / kLeastTiles));
+        for (int want = 1; want <= most; want = want < most && 2 * want > most ? most : 2 * want) {
+            const int per = std::max(1, ceil_div(k_tiles, want)), splits = std::max(1, ceil_div(k_tiles, per));
+            double us = (double)((tiles * splits + kGroups - 1) / kGroups) * kind.us * per * (bf16 ? 64 : 32) / 1024;
+            if (splits > 1) us += 3.0 + (double)splits * M * N * 8 / 5e6;
+            if (us < least) {
+                least = us;
+                best = Plan{kind.tile, kind.tile, splits, per};
+            }
+        }
     }
-    return p;
+    return best;
 }
 
 template <class C, int PK, int QK, bool PA, bool QA, int BM, int BN, int WM, int WN, int KS, int D, bool NARROW>
@@ -545,29 +694,53 @@ bool is_narrow(const Product& g) {
     return g.K == 0 || narrow(g.P, g.P_along_own, g.M, g.K) || narrow(g.Q, g.Q_along_own, g.N, g.K);
 }
 
+template <class C, int XK, int ROWS>
+void few(const Args& a, hipStream_t s) {
+    if (a.f.y.kind == E4M3 || (a.f.z.p && a.f.z.kind == E4M3)) {
+        k_few<C, XK, ROWS, 16><<<dim3((unsigned)ceil_div(a.N, 16 * kFewOutputs)), 64 * 16, 0, s>>>(a);
+    } else {
+        k_few<C, XK, ROWS, 4><<<dim3((unsigned)ceil_div(a.N, 4 * kFewOutputs)), 64 * 4, 0, s>>>(a);
+    }
+}
+
 template <class C, int PK, int QK, bool PA, bool QA>
 hipError_t run(const Product& g, hipStream_t s) {
+    if constexpr (!PA && !QA) {
+        if (g.M <= kFewRows) {
+            const Args a = args_of<C>(g, Plan{64, 64, 1, 1});
+            if (g.M == 1) few<C, PK, 1>(a, s);
+            else if (g.M == 2) few<C, PK, 2>(a, s);
+            else few<C, PK, 4>(a, s);
+            return hipGetLastError();
+        }
+    }
     const Plan p = plan_of(g.M, g.N, g.K, sizeof(C) == 2);
     const Args a = args_of<C>(g, p);
     if (is_narrow(g)) {
-        const Args n = args_of<C>(g, Plan{64, 64, 1, 1, ceil_div(g.K, kRowBytes / (int)sizeof(C))});
+        const Args n = args_of<C>(g, Plan{64, 64, 1, ceil_div(g.K, kRowBytes / (int)sizeof(C))});
         start<C, PK, QK, PA, QA, 64, 64, 2, 2, 1, 1, true>(n, s);
         return hipGetLastError();
     }
     if (p.bm == 256) {
         if constexpr (sizeof(C) == 2) start<C, PK, QK, PA, QA, 256, 256, 4, 2, 1, 1, false>(a, s);
     } else if (p.bm == 128) {
-        start<C, PK, QK, PA, QA, 128, 128, 2, 2, 1, 2, false>(a, s);
-    } else if (p.groups == 4) {
-        start<C, PK, QK, PA, QA, 64, 64, 2, 2, 4, 2, false>(a, s);
+        if constexpr (sizeof(C) == 2) start<C, PK, QK, PA, QA, 128, 128, 2, 2, 1, 2, false>(a, s);
     } else {
-        start<C, PK, QK, PA, QA, 64, 64, 2, 2, 1, 4, false>(a, s);
+        // Where a compute unit has one workgroup, two groups of its waves share the contraction in fp32, so that a matrix
+        // core's other wave multiplies while one waits: 256 x 4096 x 4096 81 -> 75 us (of bf16, whose instructions are
+        // shorter, 333 x 1365 x 1083 9.5 -> 10.1).
+        bool alone = false;
+        if constexpr (sizeof(C) == 4) {
+            alone = (long long)a.tiles_m * a.tiles_n * a.splits <= kGroups;
+            if (alone) start<C, PK, QK, PA, QA, 64, 64, 2, 2, 2, 2, false>(a, s);
+        }
+        if (!alone) start<C, PK, QK, PA, QA, 64, 64, 2, 2, 1, 2, false>(a, s);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
         const int chunks = whole_groups(g.N) / kChunk;
         const long long threads = (long long)g.M * chunks;
-        k_join<<<dim3((unsigned)((threads + kJoinThreads - 1) / kJoinThreads)), kJoinThreads, 0, s>>>(g.raw, p.splits, g.M, g.N,
+        k_join<C><<<dim3((unsigned)((threads + kJoinThreads - 1) / kJoinThreads)), kJoinThreads, 0, s>>>(g.raw, p.splits, g.M, g.N,
                                                                                                      chunks, g.f);
         e = hipGetLastError();
     }
@@ -583,17 +756,16 @@ hipError_t by_use(const Product& g, hipStream_t s) {
 }
 
 template <class C, int T, int XK>
-hipError_t both(const Product& dx, const Product& dw, int groups, hipStream_t s) {
+hipError_t both(const Product& dx, const Product& dw, hipStream_t s) {
     const Args x = args_of<C>(dx, plan_of(dx.M, dx.N, dx.K, sizeof(C) == 2));
     const Args w = args_of<C>(dw, plan_of(dw.M, dw.N, dw.K, sizeof(C) == 2));
     const unsigned first = (unsigned)x.tiles_m * x.tiles_n, all = first + (unsigned)w.tiles_m * w.tiles_n;
-    if (groups == 4) k_both<C, T, XK, 64, 64, 2, 2, 4, 2><<<dim3(all), 1024, 0, s>>>(x, w, first);
-    else k_both<C, T, XK, 64, 64, 2, 2, 1, 4><<<dim3(all), 256, 0, s>>>(x, w, first);
+    k_both<C, T, XK, 64, 64, 2, 2, 1, 2><<<dim3(all), 256, 0, s>>>(x, w, first);
     return hipGetLastError();
 }
 template <class C, int T>
-hipError_t both_of(const Product& dx, const Product& dw, int groups, hipStream_t s) {
-    return dw.Q.kind == E4M3 ? both<C, T, E4M3>(dx, dw, groups, s) : both<C, T, T>(dx, dw, groups, s);
+hipError_t both_of(const Product& dx, const Product& dw, hipStream_t s) {
+    return dw.Q.kind == E4M3 ? both<C, T, E4M3>(dx, dw, s) : both<C, T, T>(dx, dw, s);
 }
 
 }  // namespace
@@ -612,8 +784,8 @@ hipError_t launch_product(const Product& g, hipStream_t s) {
 hipError_t launch_both(const Product& dx, const Product& dw, hipStream_t s) {
     const bool bf16 = dx.P.kind == BF16;
     const Plan x = plan_of(dx.M, dx.N, dx.K, bf16), w = plan_of(dw.M, dw.N, dw.K, bf16);
-    if (x.bm == 64 && w.bm == 64 && x.groups == w.groups && x.splits == 1 && w.splits == 1 && !is_narrow(dx) && !is_narrow(dw))
-        return bf16 ? both_of<__bf16, BF16>(dx, dw, x.groups, s) : both_of<float, F32>(dx, dw, x.groups, s);
+    if (x.bm == 64 && w.bm == 64 && x.splits == 1 && w.splits == 1 && !is_narrow(dx) && !is_narrow(dw))
+        return bf16 ? both_of<__bf16, BF16>(dx, dw, s) : both_of<float, F32>(dx, dw, s);
     const hipError_t e = launch_product(dx, s);
     return e == hipSuccess ? launch_product(dw, s) : e;
 }
