@@ -70,38 +70,55 @@ __device__ __forceinline__ int scale_byte(float m) {
 __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((unsigned)byte << 23); }
 __device__ __forceinline__ float finite_magnitude(float v) {
     const float a = fabsf(v);
-    return a < __builtin_inff() ? a : 0.0f;          // NaN and infinities do not set a scale
+    return a < __builtin_inff() ? a : 0.0f;
 }
 // Largest of the four lanes of a quad (all of them active).
-__device__ __forceinline__ float quad_max(float m) {
-    m = fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, m), 0xB1, 0xF, 0xF, true)));
-    return fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, m), 0x4E, 0xF, 0xF, true)));
+__device__ __forceinline__ unsigned quad_max(unsigned m) {
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));
+    return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));
 }
-// One value in units of its group's scale, ready for the conversion (which rounds to nearest even).
-__device__ __forceinline__ float scaled_value(float v, float inverse, float most) {
-    const float s = fminf(fmaxf(v * inverse, -most), most);
-    return fabsf(v) < __builtin_inff() ? s : __builtin_nanf("");
-}
-__device__ __forceinline__ v2u eight_codes(const float (&v)[8], int byte) {
-    const float inverse = scale_value(254 - byte);
-    const float most = byte == 247 ? 240.0f : 448.0f;          // 256 * 2^120 would be no finite number
+__device__ __forceinline__ v2u convert_eight(const float (&v)[8]) {
     int w[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        int r = 0;
-        r = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_value(v[4 * h], inverse, most), scaled_value(v[4 * h + 1], inverse, most), r, false);
-        r = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_value(v[4 * h + 2], inverse, most), scaled_value(v[4 * h + 3], inverse, most), r, true);
-        w[h] = r;
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h], v[4 * h + 1], 0, false);
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2], v[4 * h + 3], w[h], true);
     }
     return v2u{(unsigned)w[0], (unsigned)w[1]};
+}
+constexpr int kLargestScale = 247;          // of the largest finite numbers
+// Codes (rounded to nearest even) and scale of a group's chunk.  The largest of the values' bits without their signs tells what
+// the group holds: with every value finite and a scale below the largest no product with the scale's reciprocal passes
+// 448 and there is nothing to look at value by value, which would take twice the instructions.
+__device__ __forceinline__ v2u eight_codes(const float (&v)[8], int& byte) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    byte = scale_byte(__uint_as_float(quad_max(top)));
+    float s[8];
+    if (byte < kLargestScale) {
+        const float inverse = scale_value(254 - byte);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = v[i] * inverse;
+    } else {
+        unsigned finite = 0;                  // NaN and infinities do not set a scale
+#pragma unroll
+        for (int i = 0; i < 8; ++i) finite = max(finite, __float_as_uint(finite_magnitude(v[i])));
+        byte = scale_byte(__uint_as_float(quad_max(finite)));
+        const float inverse = scale_value(254 - byte);
+        const float most = byte == kLargestScale ? 240.0f : 448.0f;      // 256 * 2^120 would be no finite number
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = fminf(fmaxf(v[i] * inverse, -most), most);
+            s[i] = fabsf(v[i]) < __builtin_inff() ? a : __builtin_nanf("");
+        }
+    }
+    return convert_eight(s);
 }
 // Chunk `col` (a multiple of 8) of a row in 8 bits.  The four lanes of a quad hold the four chunks of a group and all call this;
 // values past the last column are zero.  live: the chunk's group begins inside the row, so its memory is there.
 __device__ __forceinline__ void store_eight(uint8_t* codes, uint8_t* scales, int col, const float (&v)[8], bool live) {
-    float m = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_magnitude(v[i]));
-    const int byte = scale_byte(quad_max(m));
+    int byte;
     const v2u w = eight_codes(v, byte);
     if (live) {
         *as_global<v2u>(codes + col) = w;

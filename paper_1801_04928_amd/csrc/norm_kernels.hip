@@ -52,6 +52,15 @@ __device__ __forceinline__ void load_gain(const float* gain, int col, int n, flo
     }
 }
 
+// 1 / sqrt(m) to half an ulp: the instruction's value (good to one) and a Newton step whose remainder 1 - m r^2 keeps what m r
+// loses in rounding.  A row's values share it, and those kept in 8 bits next to a rounding border show its last bit.
+__device__ __forceinline__ float inverse_root(float m) {
+    if (!(m > 0x1p-100f && m < 0x1p+120f)) return 1.0f / sqrtf(m);
+    const float r = __builtin_amdgcn_rsqf(m), t = m * r;
+    const float rest = fmaf(-t, r, 1.0f) - fmaf(m, r, -t) * r;
+    return fmaf(0.5f * r, rest, r);
+}
+
 // TPR threads hold a row, NCH chunks of eight values each: a row is read once.  AGAIN: rows wider than TPR * NCH chunks are
 // read a second time for the outputs.
 template <int T, int OUT, int TPR, int NCH, bool AGAIN, bool NARROW>
@@ -95,7 +104,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_norm_forwar
 #pragma unroll
                 for (int i = 0; i < 8; ++i) square = fmaf(v[j][i], v[j][i], square);
         }
-        const float rstd = 1.0f / sqrtf(row_sum<TPR>(square, shared) / (float)a.cols + a.eps);
+        const float rstd = inverse_root(row_sum<TPR>(square, shared) / (float)a.cols + a.eps);
         if (a.rstd && t == 0) a.rstd[row] = rstd;
         for (int turn = 0; turn < turns; ++turn) {
             if constexpr (AGAIN) load(turn, v);
@@ -359,16 +368,18 @@ __global__ __launch_bounds__(kThreads) void k_slope(const Slope a, int rows_per_
     }
 }
 
-// Sums of partial rows: 64 columns a block, 16 threads a column, each over every sixteenth row.
-constexpr int kFinishCols = 64, kFinishWays = 16;
+// Sums of partial rows: 32 columns a block, 32 threads a column, each over every 32nd row with eight loads under way.
+constexpr int kFinishCols = 32, kFinishWays = 32;
 __global__ __launch_bounds__(kFinishCols * kFinishWays) void k_column_finish(const float* partial, int partials, int cols,
                                                                              float* out) {
     __shared__ float ways[kFinishWays][kFinishCols];
     const int c = threadIdx.x % kFinishCols, way = threadIdx.x / kFinishCols;
     const int col = blockIdx.x * kFinishCols + c;
     float v = 0.0f;
-    if (col < cols)
+    if (col < cols) {
+#pragma unroll 8
         for (int p = way; p < partials; p += kFinishWays) v += partial[(size_t)p * cols + col];
+    }
     ways[way][c] = v;
     __syncthreads();
     if (way == 0 && col < cols) {

@@ -321,9 +321,10 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, C* l
     typedef Tile<C, QK, Q_ALONG, BN, kThreads, NARROW> TQ;
     constexpr int BK = TP::BK, MT = BM / WM / 32, NT = BN / WN / 32;
     static_assert(D == 1 || D == 2, "a k-tile's registers and buffer are known when it is compiled");
-    // the epilogue's staging, half of the waves in either buffer: as many rows of a wave's own as fit
-    constexpr int kStageLd = NT * 32 + 4, kHalf = WM * WN / 2, kFit = kLdsElems<C, BM, BN, KS> * (int)sizeof(C) / (kHalf * kStageLd * 4);
-    constexpr int kStageRows = kFit >= 32 ? 32 : 16;
+    // the epilogue's staging, half of the waves in either buffer: as many rows of a wave's own as fit, with groups half of what
+    // is divided between them
+    constexpr int kStageLd = NT * 32 + 4, kHalf = KS == 1 ? WM * WN / 2 : WM * WN * KS;
+    constexpr int kFit = kLdsElems<C, BM, BN, KS> * (int)sizeof(C) / (kHalf * kStageLd * 4), kUnitRows = KS == 1 && kFit >= 32 ? 32 : 16;
     static_assert(kFit >= 16, "the staging fits");
 
     const int t = threadIdx.x % kThreads, group = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
@@ -475,38 +476,58 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, C* l
         __syncthreads();          // the buffers become the epilogue's
     }
     if constexpr (kChains == 2) acc[0][0][0] += acc[0][0][1];
-    if constexpr (KS > 1) {
-        // the first group adds the others' sums, in their order, and finishes the tile
-        static_assert(KS <= 4 && kThreads * MT * NT * 16 * (KS - 1) * 4 <= 3 * kLdsElems<C, BM, BN, KS> * (int)sizeof(C) / 4, "");
+    // Accumulator element e of lane (r32, half) of square (i, j) is C[.. 32 i + 8 (e / 4) + 4 half + e % 4][.. 32 j + r32]: of a wave's
+    // rows, unit u, rows kUnitRows u and on, is kElems elements of every square in a row of them.
+    constexpr int kUnits = MT * 32 / kUnitRows / KS, kElems = kUnitRows / 2;
+    float own[kUnits][NT][kElems];
+    const auto element = [&](int u, int j, int e) {
+        return acc[u * kUnitRows / 32][j][0][u * kUnitRows % 32 / 2 + e];
+    };
+    if constexpr (KS == 1) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < kElems; ++e) own[u][j][e] = element(u, j, e);
+    } else {
+        // of two groups' sums each finishes half: it gives the other half away and adds what it gets
+        static_assert(KS == 2 && 2 * kUnits * NT * kElems * kThreads * 4 <= kLdsElems<C, BM, BN, KS> * (int)sizeof(C), "the sums fit");
         v4f* sums = reinterpret_cast<v4f*>(lds0);
-        for (int k = 0; k < KS - 1; ++k) {
+        constexpr int kVecs = kElems / 4, kAll = kUnits * NT * kVecs * kThreads;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                v4f& at = sums[(k * 4 + u) * kThreads + t];
-                const v16f s = acc[0][0][0];
-                if (group == k + 1) at = v4f{s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]};
-            }
-        }
+        for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v) {
+                    v4f give;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float low = element(u, j, 4 * v + e), high = element(u + kUnits, j, 4 * v + e);
+                        own[u][j][4 * v + e] = group == 0 ? low : high;
+                        give[e] = group == 0 ? high : low;
+                    }
+                    sums[group * kAll + ((u * NT + j) * kVecs + v) * kThreads + t] = give;
+                }
         __syncthreads();
-        if (group > 0) return;
 #pragma unroll
-        for (int k = 0; k < KS - 1; ++k)
+        for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const v4f s = sums[(k * 4 + u) * kThreads + t];
+            for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[0][0][0][4 * u + e] += s[e];
-            }
-        lds0 += (KS - 1) * kThreads * 16 * (int)(sizeof(float) / sizeof(C));
+                for (int v = 0; v < kVecs; ++v) {
+                    const v4f got = sums[(1 - group) * kAll + ((u * NT + j) * kVecs + v) * kThreads + t];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) own[u][j][4 * v + e] += got[e];
+                }
     }
 
-    // Accumulator element e of lane (r32, half) of tile (i, j) is C[.. 32 i + 8 (e / 4) + 4 half + e % 4][.. 32 j + r32].  Rows turn
-    // through LDS, so that a lane holds eight consecutive columns.
-    const int r32 = lane & 31, half = lane >> 5;
-    // in LDS of the wave's own: nobody waits
-    float* stage = reinterpret_cast<float*>(wave < kHalf ? lds0 : lds1) + wave % kHalf * (kStageRows * kStageLd);
+    // Rows turn through LDS, the wave's own, so that a lane holds eight consecutive columns; nobody waits.  (With groups all of it
+    // in the second buffer: the first still holds sums.)
+    const int r32 = lane & 31, half = lane >> 5, of_all = group * WM * WN + wave;
+    float* stage = reinterpret_cast<float*>(KS == 1 && of_all < kHalf ? lds0 : lds1) + (KS == 1 ? of_all % kHalf : of_all) * (kUnitRows * kStageLd);
     constexpr int kAcross = NT * 4, kDown = 64 / kAcross;      // lanes along a row, rows at once
-    constexpr int kElems = kStageRows / 2;                     // accumulator elements that hold these rows
     const int n = n0 + wn + lane % kAcross * kChunk, n_there = min(max(g.N - n, 0), kChunk);
     // the column stays the same: its bias is loaded once; a residual is under way while the rows before it are finished
     float bias[8];
@@ -517,36 +538,34 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, C* l
         for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int u = 0; u < kUnits; ++u) {
 #pragma unroll
-        for (int h = 0; h < 16 / kElems; ++h) {
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 0; e < kElems; ++e)
-                    stage[(8 * (e >> 2) + 4 * half + (e & 3)) * kStageLd + 32 * j + r32] = acc[i][j][0][kElems * h + e];
-            __builtin_amdgcn_wave_barrier();
-            // (one copy of what follows in the code: an epilogue unrolled is larger than the instruction cache)
-            const int first = m0 + wm + 32 * i + kStageRows * h;
-            float residual[8];
-            load_residual<C>(g.f, g.M, first + lane / kAcross, n, n_there, residual);
+            for (int e = 0; e < kElems; ++e)
+                stage[(8 * (e >> 2) + 4 * half + (e & 3)) * kStageLd + 32 * j + r32] = own[u][j][e];
+        __builtin_amdgcn_wave_barrier();
+        // (one copy of what follows in the code: an epilogue unrolled is larger than the instruction cache)
+        const int first = m0 + wm + kUnitRows * (group * kUnits + u);
+        float residual[8];
+        load_residual<C>(g.f, g.M, first + lane / kAcross, n, n_there, residual);
 #pragma unroll 1
-            for (int row = lane / kAcross; row < kStageRows; row += kDown) {
-                const int col = lane % kAcross * kChunk, m = first + row;
-                const v4f lo = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col);
-                const v4f hi = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col + 4);
-                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, r[8];
+        for (int row = lane / kAcross; row < kUnitRows; row += kDown) {
+            const int col = lane % kAcross * kChunk, m = first + row;
+            const v4f lo = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col);
+            const v4f hi = *reinterpret_cast<const v4f*>(stage + row * kStageLd + col + 4);
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, r[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) r[u] = residual[u];
-                load_residual<C>(g.f, g.M, row + kDown < kStageRows ? m + kDown : g.M, n, n_there, residual);
-                if (g.splits > 1) {
-                    if (m < g.M && n_there > 0) store_values(g.raw + ((size_t)split * g.M + m) * g.N + n, n_there, v);
-                } else {
-                    finish_chunk(g.f, g.M, g.N, m, n, v, bias, r);
-                }
+            for (int i = 0; i < 8; ++i) r[i] = residual[i];
+            load_residual<C>(g.f, g.M, row + kDown < kUnitRows ? m + kDown : g.M, n, n_there, residual);
+            if (g.splits > 1) {
+                if (m < g.M && n_there > 0) store_values(g.raw + ((size_t)split * g.M + m) * g.N + n, n_there, v);
+            } else {
+                finish_chunk(g.f, g.M, g.N, m, n, v, bias, r);
             }
-            __builtin_amdgcn_wave_barrier();
         }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 template <class C, int PK, int QK, bool P_ALONG, bool Q_ALONG, int BM, int BN, int WM, int WN, int KS, int D, bool NARROW>
@@ -721,20 +740,21 @@ hipError_t run(const Product& g, hipStream_t s) {
         start<C, PK, QK, PA, QA, 64, 64, 2, 2, 1, 1, true>(n, s);
         return hipGetLastError();
     }
+    // Where a compute unit has one workgroup, two groups of waves share its contraction, so that a matrix core's other wave
+    // multiplies while one waits, and divide the epilogue.  One group -> two, us: fp32 256 x 4096 x 4096 82 -> 75; bf16 256 x
+    // 4096 x 4096 19.7 -> 17.2, 768 x 4096 x 4096 36.7 -> 34.5, 512 x 8192 x 8192 in 8 bits 86.6 -> 79.  With more workgroups
+    // than that (fp32 1024 x 2048 x 2048: 66.6 -> 66.2) there is another wave anyway.
+    const bool alone = (long long)a.tiles_m * a.tiles_n * a.splits <= kGroups;
     if (p.bm == 256) {
         if constexpr (sizeof(C) == 2) start<C, PK, QK, PA, QA, 256, 256, 4, 2, 1, 1, false>(a, s);
     } else if (p.bm == 128) {
-        if constexpr (sizeof(C) == 2) start<C, PK, QK, PA, QA, 128, 128, 2, 2, 1, 2, false>(a, s);
-    } else {
-        // Where a compute unit has one workgroup, two groups of its waves share the contraction in fp32, so that a matrix
-        // core's other wave multiplies while one waits: 256 x 4096 x 4096 81 -> 75 us (of bf16, whose instructions are
-        // shorter, 333 x 1365 x 1083 9.5 -> 10.1).
-        bool alone = false;
-        if constexpr (sizeof(C) == 4) {
-            alone = (long long)a.tiles_m * a.tiles_n * a.splits <= kGroups;
-            if (alone) start<C, PK, QK, PA, QA, 64, 64, 2, 2, 2, 2, false>(a, s);
+        if constexpr (sizeof(C) == 2) {
+            if (alone) start<C, PK, QK, PA, QA, 128, 128, 2, 2, 2, 1, false>(a, s);
+            else start<C, PK, QK, PA, QA, 128, 128, 2, 2, 1, 2, false>(a, s);
         }
-        if (!alone) start<C, PK, QK, PA, QA, 64, 64, 2, 2, 1, 2, false>(a, s);
+    } else {
+        if (alone) start<C, PK, QK, PA, QA, 64, 64, 2, 2, 2, 2, false>(a, s);
+        else start<C, PK, QK, PA, QA, 64, 64, 2, 2, 1, 2, false>(a, s);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {

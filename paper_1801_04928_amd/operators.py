@@ -217,6 +217,10 @@ def _vector(name, x, n, gpu) -> int:
     return x.data_ptr()
 
 
+def _address(x) -> int:
+    return 0 if x is None else x.data_ptr()
+
+
 class _Operator:
     """What the operators below share: device, storage type, outputs, workspace."""
 
@@ -277,7 +281,7 @@ class RmsNorm(_Operator):
         t = _torch()
         self.cols, self.eps = cols, eps
         f32 = dict(dtype=t.float32, device=self.device)
-        self.gain = t.ones(cols, **f32)
+        self.gain = t.ones(cols, **f32)          # (checked when it is set, not in every pass)
         self._sum = self._y = self._dx = self.sum = self.y = self.dx = self.rstd = self.dgain = None
         if self._forward:
             self._sum = self._new("sum", rows, cols, self.dtype if sum is None else sum)
@@ -289,6 +293,15 @@ class RmsNorm(_Operator):
             self.workspace_bytes = lf_norm_workspace_bytes(rows, cols)
             self._workspace = self._scratch(self.workspace_bytes)
 
+    @property
+    def gain(self):
+        return self._gain
+
+    @gain.setter
+    def gain(self, gain):
+        _vector("gain", gain, self.cols, self._gpu)
+        self._gain = gain
+
     def forward(self, x, branch=None):
         n, c, gpu, m = self._begin(x, self._forward, "forward"), self.cols, self._gpu, self._in
         self.sum, msum = self._some("sum", self._sum, n)
@@ -296,8 +309,7 @@ class RmsNorm(_Operator):
         self.rstd = self._rstd if n == self.rows else self._rstd[:n]
         shape = (n, c)
         st = _lib().lf_norm_forward(n, c, _matrix("x", x, shape, gpu, m[0]), _matrix("branch", branch, shape, gpu, m[1]),
-                                    _vector("gain", self.gain, c, gpu), self.eps, msum, my, self._rstd.data_ptr(),
-                                    _stream(gpu))
+                                    _address(self._gain), self.eps, msum, my, self._rstd.data_ptr(), _stream(gpu))
         return self.y if st == LF_OK else _fail(st)
 
     def backward(self, dy, dsum=None, stored=None, rstd=None):
@@ -308,7 +320,7 @@ class RmsNorm(_Operator):
         self.dx, mdx = self._some("dx", self._dx, n)
         shape = (n, c)
         st = _lib().lf_norm_backward(n, c, _matrix("dy", dy, shape, gpu, m[0]), _matrix("stored", stored, shape, gpu, m[1]),
-                                     _vector("gain", self.gain, c, gpu), _vector("rstd", rstd, n, gpu),
+                                     _address(self._gain), _vector("rstd", rstd, n, gpu),
                                      _matrix("dsum", dsum, shape, gpu, m[2]), mdx, self.dgain.data_ptr(),
                                      self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
         return self.dx if st == LF_OK else _fail(st)
@@ -330,7 +342,7 @@ class Linear(_Operator):
         t = _torch()
         self.outputs, self.inputs, self._act = outputs, inputs, ACTIVATIONS[act]
         self.w = self.b = self._mw = self.y = self.z = self.dx = self.dw = self.db = None
-        self._pb = nbytes = 0
+        nbytes = 0
         if self._forward:
             self._y = self._new("y", rows, outputs, self.dtype if y is None else y)
             self._z = self._new("z", rows, outputs, z)
@@ -352,14 +364,19 @@ class Linear(_Operator):
         if w.dtype != self.dtype:
             raise LfError(LF_EINVAL, f"w: {self.dtype} is needed, got {w.dtype}")
         m = _matrix("w", w, (self.outputs, self.inputs), self._gpu, lf_matrix())
-        self._pb = _vector("b", b, self.outputs, self._gpu)
+        _vector("b", b, self.outputs, self._gpu)
         self.w, self.b, self._mw = w, b, m
+
+    def _weights(self):
+        if self._mw is not None:
+            self._mw.data = self.w.data_ptr()          # (of w's storage as it is now)
+        return self._mw
 
     def forward(self, x, residual=None):
         n, o, i, gpu, m = self._begin(x, self._forward, "forward"), self.outputs, self.inputs, self._gpu, self._in
         self.y, my = self._some("y", self._y, n)
         self.z, mz = self._some("z", self._z, n)
-        st = _lib().lf_linear_forward(n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._mw, self._pb, self._act,
+        st = _lib().lf_linear_forward(n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._weights(), _address(self.b), self._act,
                                       _matrix("residual", residual, (n, o), gpu, m[1]), my, mz,
                                       self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
         return self.y if st == LF_OK else _fail(st)
@@ -370,6 +387,6 @@ class Linear(_Operator):
         self.dx, mdx = self._some("dx", self._dx, n)
         st = _lib().lf_linear_backward(n, o, i, _matrix("dy", dy, (n, o), gpu, m[0]),
                                        _matrix("z", self.z if z is None else z, (n, o), gpu, m[1]), self._act,
-                                       _matrix("x", x, (n, i), gpu, m[2]), self._mw, mdx, self._whole["dw"],
+                                       _matrix("x", x, (n, i), gpu, m[2]), self._weights(), mdx, self._whole["dw"],
                                        self.db.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
         return self.dx if st == LF_OK else _fail(st)

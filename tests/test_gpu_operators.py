@@ -369,6 +369,55 @@ def test_linear_backward(shape, dtype):
             assert (got[:o] == MARK).all()
 
 
+# Sizes that the tiles of 256 and 128 take, with ends in every direction and rows at odd addresses; a contraction split over
+# workgroups; up to four rows; one row of tiles more than the compute units take at once.
+LARGE = [(4090, 4083, 203), (4096, 4104, 136), (2050, 2040, 520), (1030, 1000, 4200), (3, 515, 1100), (4, 4097, 777), (2, 100, 5),
+         (260, 8200, 328)]
+
+
+def oracle_product(p, q):
+    """p q^T in 64 bits on the GPU, of operands laid out whole."""
+    return torch.mm(p.double().contiguous(), q.double().t().contiguous())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kept", [False, True], ids=["stored", "8bit"])
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+def test_linear_large(shape, kept, dtype):
+    rows, o, i = shape
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(rows + o + i)
+
+    def normal(*size, std=1.0):
+        return (torch.randn(*size, generator=g, device=DEV) * std).to(t)
+
+    # rows one element longer than what is used: no row but the first begins at a multiple of 16 bytes
+    x, w, dy = normal(rows, i + 1)[:, :i], normal(o, i + 1, std=i ** -0.5)[:, :i], normal(rows, o + 1)[:, :o]
+    bias, residual = normal(o).float(), normal(rows, o)
+    xk = P.E4M3Matrix(rows, i, device=DEV).save(x) if kept else x
+    xv = xk.load(dtype="f32") if kept else x.float()
+    p = P.Linear(rows, o, i, dtype, act="relu", z="e4m3" if kept else dtype, dw="f32", device=DEV)
+    p.set_params(w, bias)
+    y = p.forward(xk, residual)
+    z = oracle_product(xv, w) + bias.double()
+    size = oracle_product(xv.abs(), w.abs()) + bias.abs()
+    z_off = sum_error(i) * size
+    want = z.clamp(min=0) + residual.double()
+    y_off = z_off + U * (z.abs() + want.abs()) + HALF[dtype] * (want.abs() + z_off) + 1e-30
+    assert bool(((y.double() - want).abs() <= y_off).all())
+    zv = p.z.load(dtype="f32").double() if kept else p.z.double()
+    sign = zv > 0
+    dx = p.backward(dy, xk)
+    dz = torch.where(sign, dy.double(), 0.0)
+    for name, got, a, b, n, half in [("dx", dx, dz, w.t(), o, HALF[dtype]), ("dw", p.dw, dz.t(), xv.t(), rows, U)]:
+        want, size = oracle_product(a, b), oracle_product(a.abs(), b.abs())
+        off = sum_error(n) * size
+        assert bool(((got.double() - want).abs() <= off + half * (want.abs() + off) + 1e-30).all()), name
+    off = sum_error(rows) * dz.abs().sum(0) + 1e-30
+    assert bool(((p.db.double() - dz.sum(0)).abs() <= off).all())
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_activations_far_out(act):
     """Arguments from the smallest to the largest: y and the gradient before the activation, at single elements (inputs = 1)."""
