@@ -524,12 +524,12 @@ hipError_t launch_column_finish(const float* partial, int partials, int cols, fl
 }
 
 // Parts of the rows: one as long as a block's walk down all of them costs less than a second launch, then as many as give the
-// chip four blocks a compute unit.
+// chip eight blocks a compute unit (4096 x 8192: four take 1.5 us more).
 int slope_partials(int rows, int cols) {
     if (rows == 0) return 0;
     const int strips = ceil_div(cols, kWideStrip * kChunk), step = kThreads / kWideStrip * kSlopeSteps;
     if (rows <= 256) return 1;
-    return std::max(1, std::min(ceil_div(rows, step), std::max(1, 1024 / strips)));
+    return std::max(1, std::min(ceil_div(rows, step), std::max(1, 2048 / strips)));
 }
 
 hipError_t launch_slope(int rows, int cols, const Mat& dy, const Mat& z, int act, const Mat& dz, float* db, float* partial,
