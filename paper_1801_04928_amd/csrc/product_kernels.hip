@@ -311,6 +311,11 @@ __device__ __forceinline__ void interleave() {
 // Of KS groups of WM x WN waves each walks every KS-th k-tile of its workgroup's part.  D k-tiles are under way in registers,
 // one lies in LDS for the multiplications, and one is laid beside it meanwhile.  The two buffers are arrays of their own, so
 // that the compiler knows the writes to one and the reads of the other apart.
+// A wave's 64 x 128 of a 256 x 256 tile reads 6 KB of LDS for eight matrix instructions of 32 cycles, with which LDS keeps pace; 64 x
+// 64 of a 128 x 128 tile reads 4 KB for four, which takes all of LDS's time, but four times as many tiles fill the chip
+// where the matrices are smaller; 64 x 64 tiles do so for the smallest.  Measured: 4096 x 8192 x 8192 bf16 425 us = 1.29 PFLOP/s
+// (matrix cores busy 60 %), 512 x 8192 x 8192 in 8 bits 97 us = 0.71 PFLOP/s, weights from memory (34 %), 256 x 4096 x 4096 fp32 68 us
+// = 126 TFLOP/s (72 %).  Registers hold 256 x 256's sums and one k-tile under way: the early barrier's operands do not fit.
 template <class C, int BM, int BN, int KS>
 constexpr int kLdsElems = KS * (BM + BN) * (kRowBytes / (int)sizeof(C));
 
@@ -612,7 +617,9 @@ __global__ __launch_bounds__(kJoinThreads) void k_join(const float* raw, int spl
 // ================================================================================================
 // One sample, or up to four: the product is the reading of w.  A wave takes two outputs and walks their rows of w, 512 q a
 // step, with the same q of x; a workgroup's outputs are whole chunks, or whole groups of 32 (WAVES = 16) where the results
-// are kept in 8 bits.  Bound by memory: all of a wave's requests for some thousand q are under way at once.
+// are kept in 8 bits.  Bound by memory: all of a wave's requests for some thousand q are under way at once.  1 x 4096 x 4096
+// bf16: 7.3 us = 4.6 TB/s with the launch, against 14.1 with 64 x 64 tiles, split and joined.  Beyond four rows the
+// multiplications, 8 a row and value of w, would take longer than the reading.
 constexpr int kFewRows = 4, kFewOutputs = 2;
 template <class C, int XK, int ROWS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_few(const Args g) {
