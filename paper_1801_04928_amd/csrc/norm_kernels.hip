@@ -3,6 +3,7 @@
 // every value is read once, held in registers, and written once.
 #include "activation.h"
 #include "chunks.h"
+#include "column_sums.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -371,26 +372,7 @@ __global__ __launch_bounds__(kThreads) void k_slope(const Slope a, int rows_per_
     }
 }
 
-// Sums of partial rows: 32 columns a block, 32 threads a column, each over every 32nd row with eight loads under way.
-constexpr int kFinishCols = 32, kFinishWays = 32;
-__global__ __launch_bounds__(kFinishCols * kFinishWays) void k_column_finish(const float* partial, int partials, int cols,
-                                                                             float* out) {
-    __shared__ float ways[kFinishWays][kFinishCols];
-    const int c = threadIdx.x % kFinishCols, way = threadIdx.x / kFinishCols;
-    const int col = blockIdx.x * kFinishCols + c;
-    float v = 0.0f;
-    if (col < cols) {
-#pragma unroll 8
-        for (int p = way; p < partials; p += kFinishWays) v += partial[(size_t)p * cols + col];
-    }
-    ways[way][c] = v;
-    __syncthreads();
-    if (way == 0 && col < cols) {
-#pragma unroll
-        for (int i = 1; i < kFinishWays; ++i) v += ways[i][c];
-        out[col] = v;
-    }
-}
+__global__ __launch_bounds__(kFinishThreads) void k_column_finish(const ColumnSums a) { finish_columns(a, blockIdx.x); }
 
 // ================================================================================================
 // 8 bits
@@ -519,11 +501,12 @@ hipError_t launch_norm_backward(int rows, int cols, const Mat& dy, const Mat& su
         else e = sum.kind == E4M3 ? norm_backward<BF16, E4M3>(a, s) : norm_backward<BF16, BF16>(a, s);
         if (e != hipSuccess) return e;
     }
-    return dgain && !direct ? launch_column_finish(partial, norm_partials(rows, cols), cols, dgain, s) : hipSuccess;
+    return dgain && !direct ? launch_column_finish(ColumnSums{partial, norm_partials(rows, cols), cols, dgain}, s) : hipSuccess;
 }
 
-hipError_t launch_column_finish(const float* partial, int partials, int cols, float* out, hipStream_t s) {
-    k_column_finish<<<dim3(ceil_div(cols, kFinishCols)), kFinishCols * kFinishWays, 0, s>>>(partial, partials, cols, out);
+hipError_t launch_column_finish(const ColumnSums& a, hipStream_t s) {
+    if (!a.out) return hipSuccess;
+    k_column_finish<<<dim3(finish_blocks(a)), kFinishThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -536,16 +519,18 @@ int slope_partials(int rows, int cols) {
     return std::max(1, std::min(ceil_div(rows, step), std::max(1, 2048 / strips)));
 }
 
+ColumnSums slope_sums(int rows, int cols, float* db, float* partial) {
+    const int parts = slope_partials(rows, cols);
+    return ColumnSums{partial, parts, cols, parts == 1 ? nullptr : db};
+}
+
 hipError_t launch_slope(int rows, int cols, const Mat& dy, const Mat& z, int act, const Mat& dz, float* db, float* partial,
                         hipStream_t s) {
+    if (rows == 0) return hipSuccess;
     const int parts = slope_partials(rows, cols);
-    hipError_t e = hipSuccess;
-    if (rows > 0) {
-        const Slope a{rows, cols, act, dy, z, dz, !db ? nullptr : parts == 1 ? db : partial};
-        if (dy.kind == F32) e = act != NONE && z.kind == E4M3 ? slopes<F32, E4M3>(a, parts, s) : slopes<F32, F32>(a, parts, s);
-        else e = act != NONE && z.kind == E4M3 ? slopes<BF16, E4M3>(a, parts, s) : slopes<BF16, BF16>(a, parts, s);
-    }
-    return e == hipSuccess && db && parts != 1 ? launch_column_finish(partial, parts, cols, db, s) : e;
+    const Slope a{rows, cols, act, dy, z, dz, !db ? nullptr : parts == 1 ? db : partial};
+    if (dy.kind == F32) return act != NONE && z.kind == E4M3 ? slopes<F32, E4M3>(a, parts, s) : slopes<F32, F32>(a, parts, s);
+    return act != NONE && z.kind == E4M3 ? slopes<BF16, E4M3>(a, parts, s) : slopes<BF16, BF16>(a, parts, s);
 }
 
 }  // namespace ops

@@ -92,20 +92,19 @@ lf_status check_workspace(const char* call, const void* p, size_t bytes, size_t 
 
 int storage(const Mat& m) { return 1 << m.kind; }
 
-// Scratch of a product's backward pass: dz, the partial sums of db, and of the products (one after the other).
+// Scratch of a product's backward pass: dz, and the partial sums of db and of the products.
 struct Backward {
     long long dz_ld;
-    size_t dz_off, db_off, raw_off, total;
+    size_t dz_off, db_off, raw_x_off, raw_w_off, total;
 };
 Backward backward_layout(int rows, int outputs, int inputs, bool bf16) {
     Backward w;
     w.dz_ld = ((long long)outputs + 7) / 8 * 8;      // whole vectors, whatever dy's rows are
     w.dz_off = 0;
     w.db_off = w.dz_off + align_up((size_t)rows * w.dz_ld * (bf16 ? 2 : 4));
-    w.raw_off = w.db_off + align_up((size_t)lf::ops::slope_partials(rows, outputs) * outputs * sizeof(float));
-    const size_t raw = std::max(lf::ops::product_scratch_bytes(rows, inputs, outputs, bf16),
-                                lf::ops::product_scratch_bytes(outputs, inputs, rows, bf16));
-    w.total = w.raw_off + align_up(raw);
+    w.raw_x_off = w.db_off + align_up((size_t)lf::ops::slope_partials(rows, outputs) * outputs * sizeof(float));
+    w.raw_w_off = w.raw_x_off + align_up(lf::ops::product_scratch_bytes(rows, inputs, outputs, bf16));
+    w.total = w.raw_w_off + align_up(lf::ops::product_scratch_bytes(outputs, inputs, rows, bf16));
     return w;
 }
 bool product_sizes(int rows, int outputs, int inputs, lf_dtype dt) {
@@ -244,10 +243,13 @@ lf_status lf_linear_backward(int rows, int outputs, int inputs, const lf_matrix*
     if (made.p || db)
         LF_TRY(done(call, lf::ops::launch_slope(rows, outputs, mdy, mz, (int)act, made, db, (float*)(scratch + at.db_off), s)));
     const Mat none{nullptr, 0, nullptr, 0, 0};
-    float* const raw = (float*)(scratch + at.raw_off);
-    const lf::ops::Product gx{dz, mw, false, true, rows, inputs, outputs, {nullptr, LF_ACT_NONE, none, none, mdx}, raw};
-    const lf::ops::Product gw{dz, mx, true, true, outputs, inputs, rows, {nullptr, LF_ACT_NONE, none, none, mdw}, raw};
-    if (mdx.p && mdw.p && rows > 0) return done(call, lf::ops::launch_both(gx, gw, s));
+    float* const raw_x = (float*)(scratch + at.raw_x_off);
+    float* const raw_w = (float*)(scratch + at.raw_w_off);
+    const lf::ops::Product gx{dz, mw, false, true, rows, inputs, outputs, {nullptr, LF_ACT_NONE, none, none, mdx}, raw_x};
+    const lf::ops::Product gw{dz, mx, true, true, outputs, inputs, rows, {nullptr, LF_ACT_NONE, none, none, mdw}, raw_w};
+    const lf::ops::ColumnSums sums = lf::ops::slope_sums(rows, outputs, db, (float*)(scratch + at.db_off));
+    if (mdx.p && mdw.p && rows > 0) return done(call, lf::ops::launch_backward(gx, gw, sums, s));
+    LF_TRY(done(call, lf::ops::launch_column_finish(sums, s)));
     if (mdx.p && rows > 0) return done(call, lf::ops::launch_product(gx, s));
     if (mdw.p) return done(call, lf::ops::launch_product(gw, s));
     return LF_OK;

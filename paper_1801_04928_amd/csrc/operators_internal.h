@@ -30,15 +30,21 @@ hipError_t launch_norm_forward(int rows, int cols, const Mat& x, const Mat& bran
 int norm_partials(int rows, int cols);
 hipError_t launch_norm_backward(int rows, int cols, const Mat& dy, const Mat& sum, const float* gain, const float* rstd,
                                 const Mat& dsum, const Mat& dx, float* dgain, float* partial, hipStream_t s);
-// out[c] = sum over p of partial[p][c], p in order of a tree that `partials` alone decides
-hipError_t launch_column_finish(const float* partial, int partials, int cols, float* out, hipStream_t s);
-
-// ---- product_kernels.hip -------------------------------------------------------------------------------------------
-// dz = dy act'(z) into dz (may be absent), and db = its column sums (may be null; partial: [slope_partials(rows, cols)][cols])
+// out[c] = sum over p of partial[p][c], p in order of a tree that `partials` alone decides; nothing to do if out is null
+struct ColumnSums {
+    const float* partial;
+    int partials, cols;
+    float* out;
+};
+hipError_t launch_column_finish(const ColumnSums& a, hipStream_t s);
+// dz = dy act'(z) into dz (may be absent), and partial sums over its rows for db (may be null; partial: [slope_partials(rows,
+// cols)][cols]); what is left to do for db is slope_sums
 int slope_partials(int rows, int cols);
+ColumnSums slope_sums(int rows, int cols, float* db, float* partial);
 hipError_t launch_slope(int rows, int cols, const Mat& dy, const Mat& z, int act, const Mat& dz, float* db, float* partial,
                         hipStream_t s);
 
+// ---- product_kernels.hip -------------------------------------------------------------------------------------------
 // What is done with a finished element C[m][n] of a product: bias, z kept, activation, residual, y.
 struct Finish {
     const float* bias;      // [N] or null
@@ -56,8 +62,8 @@ struct Product {
 };
 size_t product_scratch_bytes(int M, int N, int K, bool bf16);
 hipError_t launch_product(const Product& g, hipStream_t s);
-// The two products of a backward pass (the same scratch, one after the other if they use it).
-hipError_t launch_both(const Product& dx, const Product& dw, hipStream_t s);
+// The two products of a backward pass, each with scratch of its own, and what is left to do for db.
+hipError_t launch_backward(const Product& dx, const Product& dw, const ColumnSums& db, hipStream_t s);
 
 }  // namespace ops
 }  // namespace lf

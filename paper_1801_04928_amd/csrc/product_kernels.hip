@@ -6,6 +6,7 @@
 // and the matrix instructions see no difference.
 #include "activation.h"
 #include "chunks.h"
+#include "column_sums.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -581,35 +582,55 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void k_product(const Args g) {
 }
 
 // Both products of a backward pass in one launch: the first `first` workgroups take dx, the others dw.
-template <class C, int T, int XK, int BM, int BN, int WM, int WN, int KS, int D>
-__global__ __launch_bounds__(64 * WM * WN * KS) void k_both(const Args dx, const Args dw, unsigned first) {
-    __shared__ __attribute__((aligned(16))) C lds0[kLdsElems<C, BM, BN, KS>];
-    __shared__ __attribute__((aligned(16))) C lds1[kLdsElems<C, BM, BN, KS>];
-    if (blockIdx.x < first) product_tile<C, T, T, false, true, BM, BN, WM, WN, KS, D, false>(dx, blockIdx.x, lds0, lds1);
-    else product_tile<C, T, XK, true, true, BM, BN, WM, WN, KS, D, false>(dw, blockIdx.x - first, lds0, lds1);
+template <class C, int T, int XK, int B, int KS>
+__global__ __launch_bounds__(256 * KS) void k_both(const Args dx, const Args dw, unsigned first) {
+    __shared__ __attribute__((aligned(16))) C lds0[kLdsElems<C, B, B, KS>];
+    __shared__ __attribute__((aligned(16))) C lds1[kLdsElems<C, B, B, KS>];
+    if (blockIdx.x < first) product_tile<C, T, T, false, true, B, B, 2, 2, KS, 2, false>(dx, blockIdx.x, lds0, lds1);
+    else product_tile<C, T, XK, true, true, B, B, 2, 2, KS, 2, false>(dw, blockIdx.x - first, lds0, lds1);
 }
 
 // Sums of the splits' partial sums, in their order, and what follows.
-constexpr int kJoinThreads = 256;
-template <class C>
-__global__ __launch_bounds__(kJoinThreads) void k_join(const float* raw, int splits, int M, int N, int chunks, const Finish f) {
-    const long long id = (long long)blockIdx.x * kJoinThreads + threadIdx.x;
-    const long long row = id / chunks;
-    const int n = (int)(id % chunks) * kChunk;
-    const int m = row < M ? (int)row : M;                     // lanes past the end stay with their quads
-    const int there = m < M ? min(max(N - n, 0), kChunk) : 0;
+struct Join {
+    const float* raw;
+    int splits, M, N, chunks;
+    Finish f;
+};
+Join join_of(const Args& a) { return Join{a.raw, a.splits, a.M, a.N, whole_groups(a.N) / kChunk, a.f}; }
+unsigned join_blocks(const Join& a, int threads) {
+    return a.splits > 1 ? (unsigned)(((long long)a.M * a.chunks + threads - 1) / threads) : 0;
+}
+template <class C, int THREADS>
+__device__ __forceinline__ void join(const Join& a, unsigned block) {
+    const long long id = (long long)block * THREADS + threadIdx.x;
+    const long long row = id / a.chunks;
+    const int n = (int)(id % a.chunks) * kChunk;
+    const int m = row < a.M ? (int)row : a.M;                 // lanes past the end stay with their quads
+    const int there = m < a.M ? min(max(a.N - n, 0), kChunk) : 0;
     float v[8] = {}, bias[8] = {}, residual[8];
-    if (f.bias) load_values(f.bias + n, there, bias);
-    load_residual<C>(f, M, m, n, there, residual);
+    if (a.f.bias) load_values(a.f.bias + n, there, bias);
+    load_residual<C>(a.f, a.M, m, n, there, residual);
     if (there > 0) {
-        for (int p = 0; p < splits; ++p) {
+        for (int p = 0; p < a.splits; ++p) {
             float u[8];
-            load_values(raw + ((size_t)p * M + m) * N + n, there, u);
+            load_values(a.raw + ((size_t)p * a.M + m) * a.N + n, there, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += u[i];
         }
     }
-    finish_chunk(f, M, N, m, n, v, bias, residual);
+    finish_chunk(a.f, a.M, a.N, m, n, v, bias, residual);
+}
+constexpr int kJoinThreads = 256;
+template <class C>
+__global__ __launch_bounds__(kJoinThreads) void k_join(const Join a) { join<C, kJoinThreads>(a, blockIdx.x); }
+
+// What a backward pass of split products ends with, in one launch: both products' sums and those of db.
+template <class C>
+__global__ __launch_bounds__(kFinishThreads) void k_join_all(const Join dx, unsigned x_blocks, const Join dw, unsigned w_blocks,
+                                                             const ColumnSums db) {
+    if (blockIdx.x < x_blocks) join<C, kFinishThreads>(dx, blockIdx.x);
+    else if (blockIdx.x < x_blocks + w_blocks) join<C, kFinishThreads>(dw, blockIdx.x - x_blocks);
+    else finish_columns(db, blockIdx.x - x_blocks - w_blocks);
 }
 
 // ================================================================================================
@@ -765,10 +786,8 @@ hipError_t run(const Product& g, hipStream_t s) {
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
-        const int chunks = whole_groups(g.N) / kChunk;
-        const long long threads = (long long)g.M * chunks;
-        k_join<C><<<dim3((unsigned)((threads + kJoinThreads - 1) / kJoinThreads)), kJoinThreads, 0, s>>>(g.raw, p.splits, g.M, g.N,
-                                                                                                     chunks, g.f);
+        const Join j = join_of(a);
+        k_join<C><<<dim3(join_blocks(j, kJoinThreads)), kJoinThreads, 0, s>>>(j);
         e = hipGetLastError();
     }
     return e;
@@ -782,17 +801,29 @@ hipError_t by_use(const Product& g, hipStream_t s) {
     return g.Q.kind == E4M3 ? run<C, T, E4M3, true, true>(g, s) : run<C, T, T, true, true>(g, s);
 }
 
+// Both products of a backward pass side by side, then what their splits and db still need: three launches with the one
+// before, not five or six, which is most of a small pass's time.  Tiles of one size, 64 or 128, for both.
 template <class C, int T, int XK>
-hipError_t both(const Product& dx, const Product& dw, hipStream_t s) {
-    const Args x = args_of<C>(dx, plan_of(dx.M, dx.N, dx.K, sizeof(C) == 2));
-    const Args w = args_of<C>(dw, plan_of(dw.M, dw.N, dw.K, sizeof(C) == 2));
-    const unsigned first = (unsigned)x.tiles_m * x.tiles_n, all = first + (unsigned)w.tiles_m * w.tiles_n;
-    k_both<C, T, XK, 64, 64, 2, 2, 1, 2><<<dim3(all), 256, 0, s>>>(x, w, first);
+hipError_t both(const Product& dx, const Plan& px, const Product& dw, const Plan& pw, const ColumnSums& db, hipStream_t s) {
+    const Args x = args_of<C>(dx, px), w = args_of<C>(dw, pw);
+    const unsigned first = (unsigned)x.tiles_m * x.tiles_n * x.splits, all = first + (unsigned)w.tiles_m * w.tiles_n * w.splits;
+    if (px.bm == 128) {
+        if constexpr (sizeof(C) == 2) k_both<C, T, XK, 128, 1><<<dim3(all), 256, 0, s>>>(x, w, first);
+    } else if (all <= kGroups) {
+        k_both<C, T, XK, 64, 2><<<dim3(all), 512, 0, s>>>(x, w, first);
+    } else {
+        k_both<C, T, XK, 64, 1><<<dim3(all), 256, 0, s>>>(x, w, first);
+    }
+    const hipError_t e = hipGetLastError();
+    const Join jx = join_of(x), jw = join_of(w);
+    const unsigned bx = join_blocks(jx, kFinishThreads), bw = join_blocks(jw, kFinishThreads), bb = finish_blocks(db);
+    if (e != hipSuccess || bx + bw + bb == 0) return e;
+    k_join_all<C><<<dim3(bx + bw + bb), kFinishThreads, 0, s>>>(jx, bx, jw, bw, db);
     return hipGetLastError();
 }
 template <class C, int T>
-hipError_t both_of(const Product& dx, const Product& dw, hipStream_t s) {
-    return dw.Q.kind == E4M3 ? both<C, T, E4M3>(dx, dw, s) : both<C, T, T>(dx, dw, s);
+hipError_t both_of(const Product& dx, const Plan& px, const Product& dw, const Plan& pw, const ColumnSums& db, hipStream_t s) {
+    return dw.Q.kind == E4M3 ? both<C, T, E4M3>(dx, px, dw, pw, db, s) : both<C, T, T>(dx, px, dw, pw, db, s);
 }
 
 }  // namespace
@@ -808,12 +839,13 @@ hipError_t launch_product(const Product& g, hipStream_t s) {
     return g.P.kind == F32 || g.Q.kind == F32 ? by_use<float, F32>(g, s) : by_use<__bf16, BF16>(g, s);
 }
 
-hipError_t launch_both(const Product& dx, const Product& dw, hipStream_t s) {
+hipError_t launch_backward(const Product& dx, const Product& dw, const ColumnSums& db, hipStream_t s) {
     const bool bf16 = dx.P.kind == BF16;
     const Plan x = plan_of(dx.M, dx.N, dx.K, bf16), w = plan_of(dw.M, dw.N, dw.K, bf16);
-    if (x.bm == 64 && w.bm == 64 && x.splits == 1 && w.splits == 1 && !is_narrow(dx) && !is_narrow(dw))
-        return bf16 ? both_of<__bf16, BF16>(dx, dw, s) : both_of<float, F32>(dx, dw, s);
-    const hipError_t e = launch_product(dx, s);
+    if (x.bm == w.bm && x.bm <= 128 && !is_narrow(dx) && !is_narrow(dw))
+        return bf16 ? both_of<__bf16, BF16>(dx, x, dw, w, db, s) : both_of<float, F32>(dx, x, dw, w, db, s);
+    hipError_t e = launch_column_finish(db, s);
+    if (e == hipSuccess) e = launch_product(dx, s);
     return e == hipSuccess ? launch_product(dw, s) : e;
 }
 
