@@ -693,32 +693,38 @@ __global__ __launch_bounds__(64 * WAVES) void k_few(const Args g) {
 }
 
 // ---- which tiles ---------------------------------------------------------------------------------------------------------
-struct Plan { int bm, bn, splits, k_tiles_per_split; };
+struct Plan {
+    int bm, bn, splits, k_tiles_per_split;
+    double us;                           // what it takes, by the measurements
+};
 constexpr int kGroups = 256;             // workgroups that fill the chip
 constexpr int kLeastTiles = 4;           // of the contraction a split has
 
-// The plan that takes the least time by the measurements: us a turn of kGroups workgroups takes for 1024 of the contraction, with 5 us
-// around; splits store their sums and read them again at 5 TB/s, in a launch more.  Measured, us, 64 | 128 | 256, bf16 rows x
-// 4096 x 4096: 256 rows 20 | 23 | 41, 512 31 | 31 | 43, 1024 55 | 41 | 55, 2048 105 | 73 | 83, 4096 205 | 138 | 117; 512 x 8192 x
-// 8192 105 | 72 | 81, 4096 x 8192 x 8192 818 | 509 | 425; 1024 x 2048 x 2048 17 | 25 | 37.
-Plan plan_of(int M, int N, int K, bool bf16) {
+// The split of a product in tiles of one size that takes the least time: a turn of kGroups workgroups takes so many us for 1024 of the
+// contraction and so many for its start and end; splits store their sums and read them again at 5 TB/s, in a launch more.
+// Measured, us, 64 | 128 | 256, bf16 4096 x 4096 x 64: 19 | 20 | 17, x 512: 40 | 33 | 28, x 4096: 205 | 138 | 117; 2048 x 2048 x 64:
+// 6.7 | 8.5 | 14, x 1024: 18 | 15 | 30; 1024 x 2048 x 2048 17 | 25 | 37; 512 x 8192 x 8192 105 | 72 | 81, 4096 x 8192 x 8192 818 | 509 | 425.
+Plan plan_with(int tile, int M, int N, int K, bool bf16) {
+    const double start = tile == 64 ? 0.85 : tile == 128 ? 3.3 : 10.5;
+    const double per_1024 = tile == 64 ? (bf16 ? 3.0 : 16.0) : tile == 128 ? 8.0 : 26.0;
     const int k_tiles = ceil_div(K, bf16 ? 64 : 32);
-    const struct { int tile; double us; } kinds[] = {{64, bf16 ? 3.1 : 16.0}, {128, 8.4}, {256, 27.0}};
-    Plan best{64, 64, 1, k_tiles};
-    double least = 1e300;
-    for (const auto& kind : kinds) {
-        if (!bf16 && kind.tile > 64) break;
-        const long long tiles = (long long)ceil_div(M, kind.tile) * ceil_div(N, kind.tile);
-        const int most = (int)std::max<long long>(1, std::min<long long>(kGroups / tiles, k_tiles / kLeastTiles));
-        for (int want = 1; want <= most; want = want < most && 2 * want > most ? most : 2 * want) {
-            const int per = std::max(1, ceil_div(k_tiles, want)), splits = std::max(1, ceil_div(k_tiles, per));
-            double us = (double)((tiles * splits + kGroups - 1) / kGroups) * kind.us * per * (bf16 ? 64 : 32) / 1024;
-            if (splits > 1) us += 3.0 + (double)splits * M * N * 8 / 5e6;
-            if (us < least) {
-                least = us;
-                best = Plan{kind.tile, kind.tile, splits, per};
-            }
-        }
+    const long long tiles = (long long)ceil_div(M, tile) * ceil_div(N, tile);
+    const int most = (int)std::max<long long>(1, std::min<long long>(kGroups / tiles, k_tiles / kLeastTiles));
+    Plan best{tile, tile, 1, k_tiles, 1e300};
+    for (int want = 1; want <= most; want = want < most && 2 * want > most ? most : 2 * want) {
+        const int per = std::max(1, ceil_div(k_tiles, want)), splits = std::max(1, ceil_div(k_tiles, per));
+        double us = (double)((tiles * splits + kGroups - 1) / kGroups) * (start + per_1024 * per * (bf16 ? 64 : 32) / 1024);
+        if (splits > 1) us += 3.0 + (double)splits * M * N * 8 / 5e6;
+        if (us < best.us) best = Plan{tile, tile, splits, per, us};
+    }
+    return best;
+}
+// 128 x 128 and 256 x 256 tiles are for bf16 (fp32 is 5 % faster with 128 from 500 of them on, and slower below).
+Plan plan_of(int M, int N, int K, bool bf16) {
+    Plan best = plan_with(64, M, N, K, bf16);
+    for (int tile = 128; bf16 && tile <= 256; tile *= 2) {
+        const Plan p = plan_with(tile, M, N, K, bf16);
+        if (p.us < best.us) best = p;
     }
     return best;
 }
@@ -754,7 +760,7 @@ template <class C, int PK, int QK, bool PA, bool QA>
 hipError_t run(const Product& g, hipStream_t s) {
     if constexpr (!PA && !QA) {
         if (g.M <= kFewRows) {
-            const Args a = args_of<C>(g, Plan{64, 64, 1, 1});
+            const Args a = args_of<C>(g, Plan{64, 64, 1, 1, 0});
             if (g.M == 1) few<C, PK, 1>(a, s);
             else if (g.M == 2) few<C, PK, 2>(a, s);
             else few<C, PK, 4>(a, s);
@@ -764,7 +770,7 @@ hipError_t run(const Product& g, hipStream_t s) {
     const Plan p = plan_of(g.M, g.N, g.K, sizeof(C) == 2);
     const Args a = args_of<C>(g, p);
     if (is_narrow(g)) {
-        const Args n = args_of<C>(g, Plan{64, 64, 1, ceil_div(g.K, kRowBytes / (int)sizeof(C))});
+        const Args n = args_of<C>(g, Plan{64, 64, 1, ceil_div(g.K, kRowBytes / (int)sizeof(C)), 0});
         start<C, PK, QK, PA, QA, 64, 64, 2, 2, 1, 1, true>(n, s);
         return hipGetLastError();
     }
@@ -841,9 +847,20 @@ hipError_t launch_product(const Product& g, hipStream_t s) {
 
 hipError_t launch_backward(const Product& dx, const Product& dw, const ColumnSums& db, hipStream_t s) {
     const bool bf16 = dx.P.kind == BF16;
-    const Plan x = plan_of(dx.M, dx.N, dx.K, bf16), w = plan_of(dw.M, dw.N, dw.K, bf16);
-    if (x.bm == w.bm && x.bm <= 128 && !is_narrow(dx) && !is_narrow(dw))
-        return bf16 ? both_of<__bf16, BF16>(dx, x, dw, w, db, s) : both_of<float, F32>(dx, x, dw, w, db, s);
+    if (!is_narrow(dx) && !is_narrow(dw)) {
+        // one tile for both saves two launches, 4 us
+        const double apart = plan_of(dx.M, dx.N, dx.K, bf16).us + plan_of(dw.M, dw.N, dw.K, bf16).us + 4.0;
+        Plan x = plan_with(64, dx.M, dx.N, dx.K, bf16), w = plan_with(64, dw.M, dw.N, dw.K, bf16);
+        if (bf16) {
+            const Plan x2 = plan_with(128, dx.M, dx.N, dx.K, true), w2 = plan_with(128, dw.M, dw.N, dw.K, true);
+            if (x2.us + w2.us < x.us + w.us) {
+                x = x2;
+                w = w2;
+            }
+        }
+        if (x.us + w.us < apart)
+            return bf16 ? both_of<__bf16, BF16>(dx, x, dw, w, db, s) : both_of<float, F32>(dx, x, dw, w, db, s);
+    }
     hipError_t e = launch_column_finish(db, s);
     if (e == hipSuccess) e = launch_product(dx, s);
     return e == hipSuccess ? launch_product(dw, s) : e;
