@@ -610,13 +610,19 @@ __device__ __forceinline__ void join(const Join& a, unsigned block) {
     float v[8] = {}, bias[8] = {}, residual[8];
     if (a.f.bias) load_values(a.f.bias + n, there, bias);
     load_residual<C>(a.f, a.M, m, n, there, residual);
-    if (there > 0) {
-        for (int p = 0; p < a.splits; ++p) {
-            float u[8];
-            load_values(a.raw + ((size_t)p * a.M + m) * a.N + n, there, u);
+    const float* at = a.raw + (size_t)m * a.N + n;
+    const size_t step = (size_t)a.M * a.N;
+    const auto add = [&](int p, int some) {
+        float u[8];
+        load_values(at + p * step, some, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += u[i];
-        }
+        for (int i = 0; i < 8; ++i) v[i] += u[i];
+    };
+    if (there == kChunk) {                // whole chunks: eight loads under way
+#pragma unroll 8
+        for (int p = 0; p < a.splits; ++p) add(p, kChunk);
+    } else if (there > 0) {
+        for (int p = 0; p < a.splits; ++p) add(p, there);
     }
     finish_chunk(a.f, a.M, a.N, m, n, v, bias, residual);
 }
