@@ -26,8 +26,10 @@
  * the largest bf16 number as 240, the number below), an infinity as a NaN.  `data`: one byte per value, 16-byte aligned,
  * ld a multiple of 32, so whole groups lie in every row's memory; what a writer leaves in the codes past the last
  * column is zero, and readers do not look at them.  `scales`: one byte e + 127 per group, scale_ld bytes from row to row.  Code times
- * scale is a bf16 number, so a matrix in 8 bits is an exact operand of bf16 and of fp32 arithmetic.  Gradients pass
- * through: the gradient with respect to a matrix in 8 bits is that with respect to its values. */
+ * scale is a bf16 number, so a matrix in 8 bits is an exact operand of bf16 and of fp32 arithmetic.  Readers also take bytes that are
+ * not written here: 255 stands for a NaN, and of bytes below 10, 0 among them, 2^(byte - 127) times a code may lie between
+ * bf16 numbers, to which bf16 operations round it.  Gradients pass through: the gradient with respect to a matrix in 8 bits
+ * is that with respect to its values. */
 #ifndef LF_OPERATORS_H
 #define LF_OPERATORS_H
 

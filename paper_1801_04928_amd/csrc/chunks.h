@@ -67,7 +67,13 @@ __device__ __forceinline__ int scale_byte(float m) {
     const int e = (int)((__float_as_uint(m) + 0x1FFFFFu) >> 23) - 8;
     return e < 10 ? 10 : e;
 }
-__device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((unsigned)byte << 23); }
+// 2^(byte - 127) of bytes from 1 to 254, and a number whose exponent says so of the two others.
+__device__ __forceinline__ float scale_power(int byte) { return __uint_as_float((unsigned)byte << 23); }
+// What any byte stands for.  This library writes 10 to 247; others' matrices may have 0, 2^-127, which is a number below the
+// normal ones, and 255, a NaN: of both the leading bit of the significand is set.
+__device__ __forceinline__ float scale_value(int byte) {
+    return __uint_as_float((unsigned)byte << 23 | ((byte + 1) & 0xFE ? 0u : 0x400000u));
+}
 __device__ __forceinline__ float finite_magnitude(float v) {
     const float a = fabsf(v);
     return a < __builtin_inff() ? a : 0.0f;
@@ -97,7 +103,7 @@ __device__ __forceinline__ v2u eight_codes(const float (&v)[8], int& byte) {
     byte = scale_byte(__uint_as_float(quad_max(top)));
     float s[8];
     if (byte < kLargestScale) {
-        const float inverse = scale_value(254 - byte);
+        const float inverse = scale_power(254 - byte);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] = v[i] * inverse;
     } else {
@@ -105,7 +111,7 @@ __device__ __forceinline__ v2u eight_codes(const float (&v)[8], int& byte) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) finite = max(finite, __float_as_uint(finite_magnitude(v[i])));
         byte = scale_byte(__uint_as_float(quad_max(finite)));
-        const float inverse = scale_value(254 - byte);
+        const float inverse = scale_power(254 - byte);
         const float most = byte == kLargestScale ? 240.0f : 448.0f;      // 256 * 2^120 would be no finite number
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

@@ -178,7 +178,7 @@ struct Tile {
             if constexpr (KIND != E4M3) {
                 *reinterpret_cast<decltype(r[u].a)*>(s + (ALONG ? at_along_i(q, i) : at_along_q(i, q / kPiece))) = r[u].a;
             } else if constexpr (sizeof(C) == 2) {
-                const float scale = scale_value(r[u].byte);
+                const float scale = scale_power(r[u].byte);          // (the instruction looks at the exponent alone)
 #pragma unroll
                 for (int h = 0; h < kPiece / 8; ++h) {
                     v8bf v;

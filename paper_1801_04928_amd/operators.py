@@ -113,7 +113,7 @@ def _storage(dtype):
 
 class E4M3Matrix:
     """rows x cols values in 8 bits: `codes` (uint8, [rows][cols rounded up to whole groups of 32], e4m3) and `scales`
-    (uint8, one power of two per group: 2^(byte - 127))."""
+    (uint8, one power of two per group: 2^(byte - 127), 255 a NaN; `save` writes 10 to 247)."""
 
     def __init__(self, rows: int, cols: int, device: str = "cuda:0"):
         t = _torch()
