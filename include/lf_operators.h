@@ -14,6 +14,7 @@
  *     nearest even.  (One rounding in between: the backward pass of a bf16 product rounds dz to bf16, for
  *     the matrix instructions take both operands in one type.)  Sums are taken in an order that the shape alone
  *     decides: the same call gives the same bits.
+ *   - hip_stream is a stream of the current device, where all buffers are.
  *   - Calls only enqueue kernels on hip_stream: no allocation, no synchronisation, no memory kept from one call to
  *     the next.  They may be recorded in a HIP graph from the first call on.  Buffers are the caller's and must live until
  *     the work has run.  `workspace` is scratch that any later call on the same stream may use again; 256-byte aligned.

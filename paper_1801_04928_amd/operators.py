@@ -2,7 +2,8 @@
 names, that marshals arguments and returns the lf_status; and objects that keep an operator's outputs and workspace, as
 `LeapfrogNet` keeps a net's.
 
-An object's outputs are overwritten by its next pass.  Work is enqueued on torch's current stream of the object's device.
+An object's outputs are overwritten by its next pass.  Work is enqueued on torch's current stream of the object's device, whatever
+the current device is.
 `rows` of an object is the most rows it takes: a call's inputs may have fewer, and its outputs then are views of the first ones."""
 from __future__ import annotations
 
@@ -152,33 +153,37 @@ class E4M3Matrix:
 
     def save(self, x) -> "E4M3Matrix":
         """Keep x ([rows][cols], f32 or bf16)."""
-        st = _lib().lf_checkpoint_save(self.rows, self.cols, _matrix("x", x, self.shape, self._gpu, self._x), self._m,
-                                       _stream(self._gpu))
-        return self if st == LF_OK else _fail(st)
+        _enqueue(self._gpu, _lib().lf_checkpoint_save, self.rows, self.cols, _matrix("x", x, self.shape, self._gpu, self._x), self._m)
+        return self
 
     def load(self, out=None, dtype="bf16"):
         """The values, in `out` or a new tensor of the type."""
         if out is None:
             out = _torch().empty(self.shape, dtype=_storage(dtype)[0], device=self.device)
-        st = _lib().lf_checkpoint_load(self.rows, self.cols, self._m, _matrix("out", out, self.shape, self._gpu, self._x),
-                                       _stream(self._gpu))
-        return out if st == LF_OK else _fail(st)
+        _enqueue(self._gpu, _lib().lf_checkpoint_load, self.rows, self.cols, self._m, _matrix("out", out, self.shape, self._gpu, self._x))
+        return out
 
 
-def _fail(st: int):
-    raise LfError(st, lf_operator_error())
+_raw_stream = _current_gpu = None
 
 
-_raw_stream = None
-
-
-def _stream(gpu: int) -> int:
-    """torch's current stream of a GPU.  (`torch.cuda.current_stream` makes an object for it: a microsecond a call.)"""
-    global _raw_stream
+def _enqueue(gpu: int, call, *args) -> None:
+    """A C call on torch's current stream of a GPU.  The GPU is the current device meanwhile: its default stream is 0, as every
+    other's is.  (`torch.cuda.current_stream` makes an object for it: a microsecond a call.)"""
+    global _raw_stream, _current_gpu
+    if gpu < 0:
+        raise LfError(LF_EINVAL, f"{call.__name__}: the operands are on the CPU, the operators run on a GPU")
     if _raw_stream is None:
-        _raw_stream = getattr(_torch()._C, "_cuda_getCurrentRawStream", None) or (
-            lambda i: _torch().cuda.current_stream(i).cuda_stream)
-    return _raw_stream(gpu) if gpu >= 0 else 0
+        t = _torch()
+        _current_gpu = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
+        _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda i: t.cuda.current_stream(i).cuda_stream)
+    if _current_gpu() == gpu:
+        st = call(*args, _raw_stream(gpu))
+    else:
+        with _torch().cuda.device(gpu):
+            st = call(*args, _raw_stream(gpu))
+    if st != LF_OK:
+        raise LfError(st, lf_operator_error())
 
 
 _TYPES = None
@@ -308,9 +313,9 @@ class RmsNorm(_Operator):
         self.y, my = self._some("out", self._y, n)
         self.rstd = self._rstd if n == self.rows else self._rstd[:n]
         shape = (n, c)
-        st = _lib().lf_norm_forward(n, c, _matrix("x", x, shape, gpu, m[0]), _matrix("branch", branch, shape, gpu, m[1]),
-                                    _address(self._gain), self.eps, msum, my, self._rstd.data_ptr(), _stream(gpu))
-        return self.y if st == LF_OK else _fail(st)
+        _enqueue(gpu, _lib().lf_norm_forward, n, c, _matrix("x", x, shape, gpu, m[0]), _matrix("branch", branch, shape, gpu, m[1]),
+                 _address(self._gain), self.eps, msum, my, self._rstd.data_ptr())
+        return self.y
 
     def backward(self, dy, dsum=None, stored=None, rstd=None):
         """From dy and the gradient that reaches the sum on other ways.  stored: the sum, if not the last forward pass's,
@@ -319,11 +324,10 @@ class RmsNorm(_Operator):
         stored, rstd = self.sum if stored is None else stored, self.rstd if rstd is None else rstd
         self.dx, mdx = self._some("dx", self._dx, n)
         shape = (n, c)
-        st = _lib().lf_norm_backward(n, c, _matrix("dy", dy, shape, gpu, m[0]), _matrix("stored", stored, shape, gpu, m[1]),
-                                     _address(self._gain), _vector("rstd", rstd, n, gpu),
-                                     _matrix("dsum", dsum, shape, gpu, m[2]), mdx, self.dgain.data_ptr(),
-                                     self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
-        return self.dx if st == LF_OK else _fail(st)
+        _enqueue(gpu, _lib().lf_norm_backward, n, c, _matrix("dy", dy, shape, gpu, m[0]), _matrix("stored", stored, shape, gpu, m[1]),
+                 _address(self._gain), _vector("rstd", rstd, n, gpu), _matrix("dsum", dsum, shape, gpu, m[2]), mdx,
+                 self.dgain.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes)
+        return self.dx
 
 
 class Linear(_Operator):
@@ -368,25 +372,25 @@ class Linear(_Operator):
         self.w, self.b, self._mw = w, b, m
 
     def _weights(self):
-        if self._mw is not None:
-            self._mw.data = self.w.data_ptr()          # (of w's storage as it is now)
+        if self._mw is None:
+            raise LfError(LF_EINVAL, "w is NULL: set_params gives the weights")
+        self._mw.data = self.w.data_ptr()          # (of w's storage as it is now)
         return self._mw
 
     def forward(self, x, residual=None):
         n, o, i, gpu, m = self._begin(x, self._forward, "forward"), self.outputs, self.inputs, self._gpu, self._in
         self.y, my = self._some("y", self._y, n)
         self.z, mz = self._some("z", self._z, n)
-        st = _lib().lf_linear_forward(n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._weights(), _address(self.b), self._act,
-                                      _matrix("residual", residual, (n, o), gpu, m[1]), my, mz,
-                                      self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
-        return self.y if st == LF_OK else _fail(st)
+        _enqueue(gpu, _lib().lf_linear_forward, n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._weights(), _address(self.b),
+                 self._act, _matrix("residual", residual, (n, o), gpu, m[1]), my, mz, self._workspace.data_ptr(),
+                 self.workspace_bytes)
+        return self.y
 
     def backward(self, dy, x, z=None):
         """From dy, the input of the forward pass, and z if it is not the last forward pass's."""
         n, o, i, gpu, m = self._begin(dy, self._backward, "backward"), self.outputs, self.inputs, self._gpu, self._in
         self.dx, mdx = self._some("dx", self._dx, n)
-        st = _lib().lf_linear_backward(n, o, i, _matrix("dy", dy, (n, o), gpu, m[0]),
-                                       _matrix("z", self.z if z is None else z, (n, o), gpu, m[1]), self._act,
-                                       _matrix("x", x, (n, i), gpu, m[2]), self._weights(), mdx, self._whole["dw"],
-                                       self.db.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes, _stream(gpu))
-        return self.dx if st == LF_OK else _fail(st)
+        _enqueue(gpu, _lib().lf_linear_backward, n, o, i, _matrix("dy", dy, (n, o), gpu, m[0]),
+                 _matrix("z", self.z if z is None else z, (n, o), gpu, m[1]), self._act, _matrix("x", x, (n, i), gpu, m[2]),
+                 self._weights(), mdx, self._whole["dw"], self.db.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes)
+        return self.dx

@@ -1,0 +1,101 @@
+"""What the operators' objects hand to the C calls (no GPU: the calls are recorded, not made)."""
+import contextlib
+import threading
+
+import pytest
+import torch
+
+import paper_1801_04928_amd as P
+from paper_1801_04928_amd import operators as ops
+
+GPU = 1
+
+
+class OnGpu(torch.Tensor):
+    """A tensor that says it is on a GPU; its address is only handed on."""
+
+    def get_device(self):
+        return GPU
+
+
+def tensor(*shape, dtype=torch.float32):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+
+
+class Calls:
+    """Stands for the library: every entry point of the operators writes down its arguments and what is current."""
+
+    def __init__(self):
+        self.made, self.current, self.before = [], 0, lambda: None
+
+    def __getattr__(self, name):
+        real = getattr(ops.lib(), name)
+        if not name.startswith("lf_") or name.endswith("_bytes") or name == "lf_operator_error":
+            return real
+
+        def call(*args):
+            self.before()
+            self.made.append((name, self.current, *[ops.lf_matrix.from_buffer_copy(a) if isinstance(a, ops.lf_matrix) else a
+                                                    for a in args]))
+            return P.LF_OK
+        call.__name__ = name
+        return call
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    c = Calls()
+    ops._lib()          # (bound before it is replaced)
+    monkeypatch.setattr(ops, "_lib", lambda: c)
+    monkeypatch.setattr(ops, "_raw_stream", lambda gpu: 0x1000 * gpu)
+    monkeypatch.setattr(ops, "_current_gpu", lambda: c.current, raising=False)
+
+    @contextlib.contextmanager
+    def device(gpu):
+        before, c.current = c.current, gpu
+        yield
+        c.current = before
+    monkeypatch.setattr(torch.cuda, "device", device)
+    return c
+
+
+def on_gpu(thing):
+    """An object that was made on the CPU, as if on the GPU."""
+    thing._gpu = GPU
+    return thing
+
+
+def linear(*args, **kwargs):
+    p = on_gpu(P.Linear(*args, device="cpu", **kwargs))
+    p.set_params(tensor(p.outputs, p.inputs), tensor(p.outputs))
+    return p
+
+
+def test_calls_are_made_on_the_objects_gpu(calls):
+    """... whichever is the current one: 0 is the default stream of any."""
+    e, n, p = on_gpu(P.E4M3Matrix(4, 40, device="cpu")), on_gpu(P.RmsNorm(4, 40, "f32", device="cpu")), linear(4, 8, 40, "f32")
+    for current in (0, GPU):
+        calls.current = current
+        calls.made.clear()
+        e.save(tensor(4, 40))
+        e.load(out=tensor(4, 40))
+        n.forward(tensor(4, 40))
+        n.backward(tensor(4, 40), stored=tensor(4, 40), rstd=tensor(4))
+        p.forward(tensor(4, 40))
+        p.backward(tensor(4, 8), tensor(4, 40))
+        assert [c[0] for c in calls.made] == ["lf_checkpoint_save", "lf_checkpoint_load", "lf_norm_forward", "lf_norm_backward",
+                                              "lf_linear_forward", "lf_linear_backward"]
+        assert all(c[1] == GPU and c[-1] == 0x1000 * GPU for c in calls.made)
+        assert calls.current == current
+
+
+def test_operands_on_the_cpu_are_refused(calls):
+    """Their addresses mean nothing to a kernel."""
+    x, e = torch.zeros(4, 40), P.E4M3Matrix(4, 40, device="cpu")
+    n, p = P.RmsNorm(4, 40, "f32", device="cpu"), P.Linear(4, 8, 40, "f32", device="cpu")
+    p.set_params(torch.zeros(8, 40))
+    for call in (lambda: e.save(x), lambda: e.load(), lambda: n.forward(x), lambda: n.backward(x, stored=x, rstd=torch.zeros(4)),
+                 lambda: p.forward(x), lambda: p.backward(torch.zeros(4, 8), x)):
+        with pytest.raises(P.LfError, match="on the CPU"):
+            call()
+    assert not calls.made
