@@ -3,7 +3,7 @@ names, that marshals arguments and returns the lf_status; and objects that keep 
 `LeapfrogNet` keeps a net's.
 
 An object's outputs are overwritten by its next pass.  Work is enqueued on torch's current stream of the object's device, whatever
-the current device is.
+the current device is.  A matrix in 8 bits may be loaded by several threads at once; any other object serves one at a time.
 `rows` of an object is the most rows it takes: a call's inputs may have fewer, and its outputs then are views of the first ones."""
 from __future__ import annotations
 
@@ -145,7 +145,6 @@ class E4M3Matrix:
         # (the stride of one row or of none says nothing)
         self._m = lf_matrix(codes.data_ptr(), max(codes.stride(0), codes.shape[1]), scales.data_ptr(),
                             max(scales.stride(0), scales.shape[1]), LF_MATRIX_E4M3)
-        self._x = lf_matrix()
 
     def first(self, rows: int) -> "E4M3Matrix":
         """The first rows (no copy)."""
@@ -153,14 +152,15 @@ class E4M3Matrix:
 
     def save(self, x) -> "E4M3Matrix":
         """Keep x ([rows][cols], f32 or bf16)."""
-        _enqueue(self._gpu, _lib().lf_checkpoint_save, self.rows, self.cols, _matrix("x", x, self.shape, self._gpu, self._x), self._m)
+        _enqueue(self._gpu, _lib().lf_checkpoint_save, self.rows, self.cols, _matrix("x", x, self.shape, self._gpu, lf_matrix()), self._m)
         return self
 
     def load(self, out=None, dtype="bf16"):
         """The values, in `out` or a new tensor of the type."""
         if out is None:
             out = _torch().empty(self.shape, dtype=_storage(dtype)[0], device=self.device)
-        _enqueue(self._gpu, _lib().lf_checkpoint_load, self.rows, self.cols, self._m, _matrix("out", out, self.shape, self._gpu, self._x))
+        _enqueue(self._gpu, _lib().lf_checkpoint_load, self.rows, self.cols, self._m,
+                 _matrix("out", out, self.shape, self._gpu, lf_matrix()))
         return out
 
 

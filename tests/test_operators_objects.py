@@ -99,3 +99,16 @@ def test_operands_on_the_cpu_are_refused(calls):
         with pytest.raises(P.LfError, match="on the CPU"):
             call()
     assert not calls.made
+
+
+def test_threads_may_load_one_matrix(calls):
+    """Each call writes to its own thread's tensor, though both have theirs ready before either is made."""
+    e = on_gpu(P.E4M3Matrix(4, 40, device="cpu"))
+    outs = [tensor(4, 40) for _ in range(2)]
+    calls.current, calls.before = GPU, threading.Barrier(2, timeout=20).wait
+    threads = [threading.Thread(target=e.load, args=(out,)) for out in outs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert sorted(c[5].data for c in calls.made) == sorted(out.data_ptr() for out in outs)
