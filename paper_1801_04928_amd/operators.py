@@ -222,8 +222,19 @@ def _vector(name, x, n, gpu) -> int:
     return x.data_ptr()
 
 
-def _address(x) -> int:
-    return 0 if x is None else x.data_ptr()
+class _Kept:
+    """A vector that an object keeps by reference: checked when it is given, and again where it has moved."""
+
+    def __init__(self, name, x, n, gpu):
+        self.name, self.n, self.gpu = name, n, gpu
+        self.at = _vector(name, x, n, gpu)
+
+    def address(self, x) -> int:
+        if x is None:
+            return 0
+        if x.data_ptr() != self.at:
+            self.at = _vector(self.name, x, self.n, self.gpu)
+        return self.at
 
 
 class _Operator:
@@ -278,7 +289,7 @@ class RmsNorm(_Operator):
 
     gain: f32 [cols], ones at first.  out: type of y, dtype or "e4m3".  After `forward`: sum, y (a tensor or an E4M3Matrix),
     rstd.  After `backward`: dx (the gradient of x and of branch), dgain.  out, sum and dx may be matrices of the caller's to
-    write to (sum: x or branch itself, too; dx: dsum itself, too); sum may be "none"."""
+    write to, which stay where they are (sum: x or branch itself, too; dx: dsum itself, too); sum may be "none"."""
 
     def __init__(self, rows: int, cols: int, dtype="bf16", out=None, eps: float = 1e-6, passes: str = "both", sum=None,
                  dx=None, device: str = "cuda:0"):
@@ -304,8 +315,7 @@ class RmsNorm(_Operator):
 
     @gain.setter
     def gain(self, gain):
-        _vector("gain", gain, self.cols, self._gpu)
-        self._gain = gain
+        self._gain, self._kept_gain = gain, _Kept("gain", gain, self.cols, self._gpu)
 
     def forward(self, x, branch=None):
         n, c, gpu, m = self._begin(x, self._forward, "forward"), self.cols, self._gpu, self._in
@@ -314,7 +324,7 @@ class RmsNorm(_Operator):
         self.rstd = self._rstd if n == self.rows else self._rstd[:n]
         shape = (n, c)
         _enqueue(gpu, _lib().lf_norm_forward, n, c, _matrix("x", x, shape, gpu, m[0]), _matrix("branch", branch, shape, gpu, m[1]),
-                 _address(self._gain), self.eps, msum, my, self._rstd.data_ptr())
+                 self._kept_gain.address(self._gain), self.eps, msum, my, self._rstd.data_ptr())
         return self.y
 
     def backward(self, dy, dsum=None, stored=None, rstd=None):
@@ -325,7 +335,7 @@ class RmsNorm(_Operator):
         self.dx, mdx = self._some("dx", self._dx, n)
         shape = (n, c)
         _enqueue(gpu, _lib().lf_norm_backward, n, c, _matrix("dy", dy, shape, gpu, m[0]), _matrix("stored", stored, shape, gpu, m[1]),
-                 _address(self._gain), _vector("rstd", rstd, n, gpu), _matrix("dsum", dsum, shape, gpu, m[2]), mdx,
+                 self._kept_gain.address(self._gain), _vector("rstd", rstd, n, gpu), _matrix("dsum", dsum, shape, gpu, m[2]), mdx,
                  self.dgain.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes)
         return self.dx
 
@@ -335,7 +345,7 @@ class Linear(_Operator):
 
     y: storage type ("f32", "bf16", None: dtype) or "e4m3"; z, what the backward pass needs of an activation:
     the same, or "none".  dw: type of the weights' gradient, dtype or "f32".  After `forward`: y, z.  After `backward`: dx, dw, db.
-    y, z, dx and dw may be matrices of the caller's to write to, workspace scratch that operators on one stream share
+    y, z, dx and dw may be matrices of the caller's to write to, which stay where they are, workspace scratch that operators on one stream share
     (uint8; `workspace_bytes` of it at least)."""
 
     def __init__(self, rows: int, outputs: int, inputs: int, dtype="bf16", act: str = "none", y=None, z="none", dx=None,
@@ -345,7 +355,7 @@ class Linear(_Operator):
             raise LfError(LF_EINVAL, f"activation {act!r}: one of {sorted(ACTIVATIONS)}")
         t = _torch()
         self.outputs, self.inputs, self._act = outputs, inputs, ACTIVATIONS[act]
-        self.w = self.b = self._mw = self.y = self.z = self.dx = self.dw = self.db = None
+        self.w = self.b = self.y = self.z = self.dx = self.dw = self.db = None
         nbytes = 0
         if self._forward:
             self._y = self._new("y", rows, outputs, self.dtype if y is None else y)
@@ -364,24 +374,26 @@ class Linear(_Operator):
 
     def set_params(self, w, b=None) -> None:
         """Register w ([outputs][inputs], storage type) and b ([outputs] f32, or None).  They are kept by reference: the
-        data may change between passes."""
+        data may change between passes, and where it lies."""
+        kept = _Kept("b", b, self.outputs, self._gpu)
+        self._check_weights(w, lf_matrix())
+        self.w, self.b, self._kept_b = w, b, kept
+
+    def _check_weights(self, w, m):
         if w.dtype != self.dtype:
             raise LfError(LF_EINVAL, f"w: {self.dtype} is needed, got {w.dtype}")
-        m = _matrix("w", w, (self.outputs, self.inputs), self._gpu, lf_matrix())
-        _vector("b", b, self.outputs, self._gpu)
-        self.w, self.b, self._mw = w, b, m
+        return _matrix("w", w, (self.outputs, self.inputs), self._gpu, m)
 
     def _weights(self):
-        if self._mw is None:
+        if self.w is None:
             raise LfError(LF_EINVAL, "w is NULL: set_params gives the weights")
-        self._mw.data = self.w.data_ptr()          # (of w's storage as it is now)
-        return self._mw
+        return self._check_weights(self.w, self._in[3])          # (as it lies now)
 
     def forward(self, x, residual=None):
         n, o, i, gpu, m = self._begin(x, self._forward, "forward"), self.outputs, self.inputs, self._gpu, self._in
         self.y, my = self._some("y", self._y, n)
         self.z, mz = self._some("z", self._z, n)
-        _enqueue(gpu, _lib().lf_linear_forward, n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._weights(), _address(self.b),
+        _enqueue(gpu, _lib().lf_linear_forward, n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._weights(), self._kept_b.address(self.b),
                  self._act, _matrix("residual", residual, (n, o), gpu, m[1]), my, mz, self._workspace.data_ptr(),
                  self.workspace_bytes)
         return self.y

@@ -112,3 +112,40 @@ def test_threads_may_load_one_matrix(calls):
     for t in threads:
         t.join()
     assert sorted(c[5].data for c in calls.made) == sorted(out.data_ptr() for out in outs)
+
+
+def given(calls, argument):
+    return calls.made[-1][2 + argument]
+
+
+def test_weights_that_have_moved_are_looked_at_again(calls):
+    """w, b and gain are kept by reference: a call takes them as they lie then, and refuses what no longer fits."""
+    p, x = linear(4, 8, 40, "f32"), tensor(4, 40)
+    for other in (torch.zeros(8, 56)[:, :40], torch.zeros(8, 40)):
+        p.w.data = other
+        p.forward(x)
+        assert (given(calls, 4).data, given(calls, 4).ld) == (other.data_ptr(), other.stride(0))
+        p.backward(tensor(4, 8), x)
+        assert (given(calls, 7).data, given(calls, 7).ld) == (other.data_ptr(), other.stride(0))
+    square = linear(4, 8, 8, "f32")
+    n = on_gpu(P.RmsNorm(4, 40, "f32", device="cpu"))
+    n.gain = tensor(40)
+    for v, name, call in ((p.b, "b", lambda: p.forward(x)), (n.gain, "gain", lambda: n.forward(x))):
+        v.data = torch.zeros(v.shape)
+        call()
+        assert v.data_ptr() in calls.made[-1]
+        made = len(calls.made)
+        v.data = torch.zeros(v.shape[0] - 1)
+        with pytest.raises(P.LfError, match=f"{name}: "):
+            call()
+        assert len(calls.made) == made
+    for w, why in ((torch.zeros(8, 39), "w: 8 x 40"), (torch.zeros(7, 40), "w: 8 x 40"), (torch.zeros(40, 8).t(), "contiguous")):
+        p.w.data = w
+        with pytest.raises(P.LfError, match=why):
+            p.forward(x)
+    square.w.data = square.w.data.t()          # (at the same address)
+    with pytest.raises(P.LfError, match="contiguous"):
+        square.forward(tensor(4, 8))
+    p.w = tensor(8, 40, dtype=torch.bfloat16)
+    with pytest.raises(P.LfError, match="w: torch.float32"):
+        p.forward(x)
