@@ -399,10 +399,12 @@ class Linear(_Operator):
         return self.y
 
     def backward(self, dy, x, z=None):
-        """From dy, the input of the forward pass, and z if it is not the last forward pass's."""
+        """From dy, the input of the forward pass, and z if it is not the last forward pass's.  Without an activation z is not
+        looked at."""
         n, o, i, gpu, m = self._begin(dy, self._backward, "backward"), self.outputs, self.inputs, self._gpu, self._in
+        z = None if self._act == LF_ACT_NONE else self.z if z is None else z
         self.dx, mdx = self._some("dx", self._dx, n)
         _enqueue(gpu, _lib().lf_linear_backward, n, o, i, _matrix("dy", dy, (n, o), gpu, m[0]),
-                 _matrix("z", self.z if z is None else z, (n, o), gpu, m[1]), self._act, _matrix("x", x, (n, i), gpu, m[2]),
+                 _matrix("z", z, (n, o), gpu, m[1]), self._act, _matrix("x", x, (n, i), gpu, m[2]),
                  self._weights(), mdx, self._whole["dw"], self.db.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes)
         return self.dx
