@@ -153,12 +153,12 @@ def test_weights_that_have_moved_are_looked_at_again(calls):
 
 def test_what_was_kept_of_another_pass_does_not_stop_one_that_needs_none_of_it(calls):
     """Without an activation the backward pass does not look at z: neither at the last forward pass's, of other rows, nor at one given."""
-    p = linear(6, 8, 40, "f32", z="f32")
+    p = linear(3, 8, 40, "f32", z="f32")
     p.z = tensor(5, 8)
     p.backward(tensor(3, 8), tensor(3, 40))
     p.backward(tensor(3, 8), tensor(3, 40), z=tensor(5, 8))
     assert len(calls.made) == 2 and given(calls, 4) is None
-    p = linear(6, 8, 40, "f32", z="f32", act="relu")
+    p = linear(3, 8, 40, "f32", z="f32", act="relu")
     p.z = tensor(5, 8)
     with pytest.raises(P.LfError, match="z: 3 x 8"):
         p.backward(tensor(3, 8), tensor(3, 40))
