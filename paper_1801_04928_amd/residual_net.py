@@ -5,7 +5,7 @@
 
 The addition that a block begins with is the norm's; the last one, which no norm follows, is the last product's.  What the
 backward pass needs of the activations -- s, h, u and the value before the activation -- is kept in 8 bits
-(checkpoints="e4m3"), half of the storage type's memory, or in the storage type."""
+(checkpoints="e4m3"), half of the storage type's memory, or in the storage type ("storage")."""
 from __future__ import annotations
 
 from .binding import LF_EINVAL, LfError
@@ -25,8 +25,8 @@ class ResidualNet:
             raise LfError(LF_EINVAL, f"{depth} blocks")
         self.torch, self.depth, self.rows = torch, depth, rows
         self.dtype, _, dt = _storage(dtype)
-        if checkpoints != "e4m3" and _storage(checkpoints)[0] != self.dtype:
-            raise LfError(LF_EINVAL, f"checkpoints = {checkpoints!r}: e4m3 or the storage type")
+        if checkpoints not in ("e4m3", "storage") and _storage(checkpoints)[0] != self.dtype:
+            raise LfError(LF_EINVAL, f"checkpoints = {checkpoints!r}: e4m3, storage or the storage type's name")
         kept = "e4m3" if checkpoints == "e4m3" else self.dtype
         new = dict(dtype=self.dtype, device=device)
         f32 = dict(dtype=torch.float32, device=device)

@@ -1,0 +1,31 @@
+"""ResidualNet and its example as far as they go without a GPU."""
+import pytest
+import torch
+
+import paper_1801_04928_amd as P
+
+
+def net(**kwargs):
+    return P.ResidualNet(2, 40, 24, 4, device="cpu", **kwargs)
+
+
+def kept(n):
+    """What the net keeps for its backward pass."""
+    return [*n._sums, *[v._y for v in n.norms], *[v._y for v in n.ups], *[v._z for v in n.ups]]
+
+
+@pytest.mark.parametrize("dtype, checkpoints", [("f32", "storage"), ("f32", "f32"), ("bf16", "storage"), ("bf16", "bf16"),
+                                                ("bf16", torch.bfloat16)])
+def test_checkpoints_in_the_storage_type(dtype, checkpoints):
+    n = net(dtype=dtype, checkpoints=checkpoints)
+    assert all(isinstance(v, torch.Tensor) and v.dtype == n.dtype for v in kept(n))
+
+
+def test_checkpoints_in_8_bits():
+    assert all(isinstance(v, P.E4M3Matrix) for v in kept(net(checkpoints="e4m3")))
+
+
+@pytest.mark.parametrize("dtype, checkpoints", [("f32", "bf16"), ("bf16", "f32"), ("f32", "e5m2")])
+def test_other_checkpoints_are_refused(dtype, checkpoints):
+    with pytest.raises(P.LfError):
+        net(dtype=dtype, checkpoints=checkpoints)
