@@ -4,8 +4,9 @@
     output:   s + the last branch
 
 The addition that a block begins with is the norm's; the last one, which no norm follows, is the last product's.  What the
-backward pass needs of the activations -- s, h, u and the value before the activation -- is kept in 8 bits
-(checkpoints="e4m3"), half of the storage type's memory, or in the storage type ("storage")."""
+backward pass needs of the activations -- s, h, u and the value before the activation -- is kept in the storage type
+(checkpoints="storage"), or in 8 bits ("e4m3"), half of bf16's memory.  In 8 bits h and u are only there as they are kept: the forward
+products' operands are in 8 bits then, too, and the net's answers are those of 8-bit activations."""
 from __future__ import annotations
 
 from .binding import LF_EINVAL, LfError
@@ -19,7 +20,7 @@ class ResidualNet:
     db2.  `forward(x)` gives the output, `backward(dy)` the gradient of x."""
 
     def __init__(self, depth: int, width: int, hidden: int, rows: int, dtype="bf16", act: str = "gelu",
-                 checkpoints="e4m3", device: str = "cuda:0"):
+                 checkpoints="storage", device: str = "cuda:0"):
         import torch
         if depth < 1:
             raise LfError(LF_EINVAL, f"{depth} blocks")

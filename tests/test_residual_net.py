@@ -29,3 +29,8 @@ def test_checkpoints_in_8_bits():
 def test_other_checkpoints_are_refused(dtype, checkpoints):
     with pytest.raises(P.LfError):
         net(dtype=dtype, checkpoints=checkpoints)
+
+
+def test_fewer_bits_only_where_they_are_asked_for():
+    """In 8 bits the forward products read what is kept, so the answers change: not by default."""
+    assert all(isinstance(v, torch.Tensor) and v.dtype == torch.bfloat16 for v in kept(net()))
