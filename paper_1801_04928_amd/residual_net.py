@@ -56,6 +56,7 @@ class ResidualNet:
             self.b2.append(torch.zeros(width, **f32))
             self.ups[b].set_params(self.w1[b], self.b1[b])
             self.downs[b].set_params(self.w2[b], self.b2[b])
+        self._masters = None
         self.gain = [n.gain for n in self.norms]
         self.dgain = [n.dgain for n in self.norms]
         self.dw1, self.db1 = [p.dw for p in self.ups], [p.db for p in self.ups]
@@ -91,8 +92,20 @@ class ResidualNet:
         return ds
 
     def descend(self, eta: float) -> None:
-        """A plain gradient-descent step: every parameter less eta times its gradient."""
-        for params, grads in ((self.w1, self.dw1), (self.w2, self.dw2), (self.b1, self.db1), (self.b2, self.db2),
-                              (self.gain, self.dgain)):
-            for p, g in zip(params, grads):
-                p.add_(g, alpha=-eta)
+        """A plain gradient-descent step: every parameter less eta times its gradient.  Weights in bf16 descend in fp32 copies, made
+        in the first step, and are these copies' roundings, so that steps smaller than half of bf16's add up.  A weight that was
+        set to something else meanwhile goes on from there."""
+        torch = self.torch
+        if self.dtype == torch.float32:
+            weights = [*self.w1, *self.w2]
+        else:
+            if self._masters is None:
+                self._masters = [w.float() for w in (*self.w1, *self.w2)]
+            weights = self._masters
+            for w, master in zip((*self.w1, *self.w2), weights):
+                master.copy_(torch.where(master.to(w.dtype) == w, master, w.float()))
+        for p, g in zip((*weights, *self.b1, *self.b2, *self.gain), (*self.dw1, *self.dw2, *self.db1, *self.db2, *self.dgain)):
+            p.add_(g, alpha=-eta)
+        for w, master in zip((*self.w1, *self.w2), weights):
+            if master is not w:
+                w.copy_(master)
