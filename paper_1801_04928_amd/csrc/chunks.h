@@ -10,10 +10,6 @@ namespace ops {
 constexpr int kGroup = 32;        // values that share a scale
 constexpr int kChunk = 8;
 
-// Vectors at any address of their elements: global memory takes wide loads and stores that are not aligned to their
-// width, so one instruction serves aligned rows and others (which cost the lines they straddle).
-typedef v4f any_v4f __attribute__((aligned(4)));
-typedef v8bf any_v8bf __attribute__((aligned(2)));
 typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 
 template <int KIND> struct Stored;
@@ -23,16 +19,29 @@ template <> struct Stored<BF16> { typedef __bf16 type; };
 template <class T> using global_ptr = T __attribute__((address_space(1)))*;
 template <class T, class U> __device__ __forceinline__ global_ptr<T> as_global(U* p) { return (global_ptr<T>)(p); }
 
+// Vectors at any address of their elements: global memory takes wide loads and stores that are not aligned to their
+// width, so one instruction serves aligned rows and others (which cost the lines they straddle).  The alignment is part of the
+// typedef, which a template's argument loses: these pointers are no template's.  (Of a load that it takes for aligned the compiler
+// makes a scalar one where the address is the same for a whole wave, and that leaves out the address's last two bits.)
+typedef v4f any_v4f __attribute__((aligned(4)));
+typedef v8bf any_v8bf __attribute__((aligned(2)));
+typedef __attribute__((address_space(1))) any_v4f* any_v4f_ptr;
+typedef __attribute__((address_space(1))) any_v8bf* any_v8bf_ptr;
+__device__ __forceinline__ v4f load_vector(const float* p) { return *(any_v4f_ptr)(const_cast<float*>(p)); }
+__device__ __forceinline__ v8bf load_vector(const __bf16* p) { return *(any_v8bf_ptr)(const_cast<__bf16*>(p)); }
+__device__ __forceinline__ void store_vector(float* p, v4f v) { *(any_v4f_ptr)(p) = v; }
+__device__ __forceinline__ void store_vector(__bf16* p, v8bf v) { *(any_v8bf_ptr)(p) = v; }
+
 // n (0..8) values from p; the others are zero.
 template <class T>
 __device__ __forceinline__ void load_values(const T* p, int n, float (&v)[8]) {
     if (n >= kChunk) {
         if constexpr (sizeof(T) == 4) {
-            const v4f a = *as_global<const any_v4f>(p), b = *as_global<const any_v4f>(p + 4);
+            const v4f a = load_vector(p), b = load_vector(p + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
         } else {
-            const v8bf a = *as_global<const any_v8bf>(p);
+            const v8bf a = load_vector(p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
         }
@@ -45,13 +54,13 @@ template <class T>
 __device__ __forceinline__ void store_values(T* p, int n, const float (&v)[8]) {
     if (n >= kChunk) {
         if constexpr (sizeof(T) == 4) {
-            *as_global<any_v4f>(p) = v4f{v[0], v[1], v[2], v[3]};
-            *as_global<any_v4f>(p + 4) = v4f{v[4], v[5], v[6], v[7]};
+            store_vector(p, v4f{v[0], v[1], v[2], v[3]});
+            store_vector(p + 4, v4f{v[4], v[5], v[6], v[7]});
         } else {
             v8bf a;
 #pragma unroll
             for (int i = 0; i < 8; ++i) a[i] = (__bf16)v[i];
-            *as_global<any_v8bf>(p) = a;
+            store_vector(p, a);
         }
     } else {
 #pragma unroll
@@ -207,10 +216,10 @@ __device__ __forceinline__ void fetch_chunk(Chunk<KIND>& c, const Mat& m, long l
         } else {
             p += min(col, cols - kChunk);
             if constexpr (KIND == F32) {
-                c.a[0] = *as_global<const any_v4f>(p);
-                c.a[1] = *as_global<const any_v4f>(p + 4);
+                c.a[0] = load_vector(p);
+                c.a[1] = load_vector(p + 4);
             } else {
-                c.a = __builtin_bit_cast(v4u, *as_global<const any_v8bf>(p));
+                c.a = __builtin_bit_cast(v4u, load_vector(p));
             }
         }
     }

@@ -102,9 +102,9 @@ struct Tile {
             const unsigned col = ALONG ? column(i0, i, I_all) : min(q0 + q, in_memory(q_end) - kPiece);
             const unsigned off = !ALONG ? at[u] + col * kElemBytes : there ? at[u] : col * kElemBytes;
             if constexpr (KIND == F32) {
-                r[u].a = *as_global<const any_v4f>(base + off);
+                r[u].a = load_vector((const float*)(base + off));
             } else if constexpr (KIND == BF16) {
-                r[u].a = __builtin_bit_cast(v4u, *as_global<const any_v8bf>(base + off));
+                r[u].a = __builtin_bit_cast(v4u, load_vector((const __bf16*)(base + off)));
             } else {
                 if constexpr (kPiece == 16) r[u].a = *as_global<const v4u>(base + off);
                 else r[u].a = *as_global<const v2u>(base + off);
