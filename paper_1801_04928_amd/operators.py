@@ -376,18 +376,22 @@ class Linear(_Operator):
         """Register w ([outputs][inputs], storage type) and b ([outputs] f32, or None).  They are kept by reference: the
         data may change between passes, and where it lies."""
         kept = _Kept("b", b, self.outputs, self._gpu)
-        self._check_weights(w, lf_matrix())
+        self._look_at(w)
         self.w, self.b, self._kept_b = w, b, kept
 
-    def _check_weights(self, w, m):
+    def _look_at(self, w):
         if w.dtype != self.dtype:
             raise LfError(LF_EINVAL, f"w: {self.dtype} is needed, got {w.dtype}")
-        return _matrix("w", w, (self.outputs, self.inputs), self._gpu, m)
+        self._mw = _matrix("w", w, (self.outputs, self.inputs), self._gpu, lf_matrix())
+        self._seen = w.data_ptr(), w.stride(), w.shape
 
     def _weights(self):
-        if self.w is None:
+        w = self.w
+        if w is None:
             raise LfError(LF_EINVAL, "w is NULL: set_params gives the weights")
-        return self._check_weights(self.w, self._in[3])          # (as it lies now)
+        if (w.data_ptr(), w.stride(), w.shape) != self._seen or w.dtype != self.dtype:
+            self._look_at(w)
+        return self._mw
 
     def forward(self, x, residual=None):
         n, o, i, gpu, m = self._begin(x, self._forward, "forward"), self.outputs, self.inputs, self._gpu, self._in

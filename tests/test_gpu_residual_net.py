@@ -25,3 +25,18 @@ def test_example_takes_its_options(dtype, checkpoints, monkeypatch, capsys):
     example().main()
     out = capsys.readouterr().out
     assert "step 2: cost" in out and "one sample" in out
+
+
+@pytest.mark.parametrize("checkpoints", ["e4m3", "storage"])
+def test_a_pass_of_no_rows(checkpoints):
+    """Nothing comes out, and the gradients, sums over no rows, are zeros whatever was there."""
+    import torch
+    import paper_1801_04928_amd as P
+    net = P.ResidualNet(2, 40, 24, 4, checkpoints=checkpoints)
+    net.init()
+    grads = [*net.dw1, *net.dw2, *net.db1, *net.db2, *net.dgain]
+    for g in grads:
+        g.fill_(7.0)
+    x = torch.ones(4, 40, dtype=torch.bfloat16, device="cuda:0")[:0]
+    assert net.forward(x).shape == (0, 40) and net.backward(x).shape == (0, 40)
+    assert all(bool((g == 0).all()) for g in grads)
