@@ -62,7 +62,7 @@ __device__ __forceinline__ float inverse_root(float m) {
     return fmaf(0.5f * r, rest, r);
 }
 
-// Bound by memory: 16384 x 8192 bf16 with y in 8 bits 167 us = 5.65 TB/s.  TPR threads hold a row, NCH chunks of eight values
+// Bound by memory: 16384 x 8192 bf16 with y in 8 bits 167 us = 5.65 TB/s, fp32 385 us = 5.6.  TPR threads hold a row, NCH chunks of eight values
 // each: a row is read once.  AGAIN: rows wider than TPR * NCH chunks are
 // read a second time for the outputs.
 template <int T, int OUT, int TPR, int NCH, bool AGAIN, bool NARROW>
@@ -137,8 +137,10 @@ struct NormBackward {
 
 // A block takes rows blockIdx.x, + gridDim.x, ...: the sums of dy h over its rows stay in registers, a row of partial sums
 // per block is all that the gain's gradient costs in memory.  The next row is under way, as it lies in memory, while one is
-// worked on (16384 x 8192 bf16, s in 8 bits: 314 -> 172 us = 5.5 TB/s).  AGAIN as in the forward pass (the gain's gradient is
-// then a kernel of its own, k_gain_gradient).
+// worked on (16384 x 8192 bf16, s in 8 bits: 314 -> 171 us = 5.5 TB/s; fp32 397 us = 5.4).  Rows of 8193 to 16384 columns take 1024
+// threads of at most 128 registers, which do not hold all that: 18 (bf16), 31 (from 8 bits), 151 (fp32) and 156 (from 8 bits) are
+// spilled, and 16384 x 16384 bf16 takes 512 us = 4.2 TB/s, 8192 x 16384 fp32 671 us = 3.2.  AGAIN as in the forward pass (the gain's
+// gradient is then a kernel of its own, k_gain_gradient).
 template <int T, int S, int TPR, int NCH, bool AGAIN, bool NARROW>
 __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_norm_backward(const NormBackward a) {
     constexpr int kBlock = TPR > kThreads ? TPR : kThreads, kRows = kBlock / TPR;

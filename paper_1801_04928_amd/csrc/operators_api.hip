@@ -235,7 +235,8 @@ lf_status lf_linear_backward(int rows, int outputs, int inputs, const lf_matrix*
     const hipStream_t s = (hipStream_t)hip_stream;
     uint8_t* const scratch = (uint8_t*)workspace;
 
-    // The gradient before the activation: made once, both products read it.
+    // The gradient before the activation: made once, both products read it.  Of bf16 operands it is rounded to bf16, one rounding more
+    // than the outputs': the matrix instructions take both operands in one type, and fp32 ones run at a tenth of the rate.
     const bool products = mdx.p || mdw.p;
     Mat dz = mdy;
     if (act != LF_ACT_NONE && products) dz = Mat{scratch + at.dz_off, at.dz_ld, nullptr, 0, mdy.kind};

@@ -314,9 +314,10 @@ __device__ __forceinline__ void interleave() {
 // that the compiler knows the writes to one and the reads of the other apart.
 // A wave's 64 x 128 of a 256 x 256 tile reads 6 KB of LDS for eight matrix instructions of 32 cycles, with which LDS keeps pace; 64 x
 // 64 of a 128 x 128 tile reads 4 KB for four, which takes all of LDS's time, but four times as many tiles fill the chip
-// where the matrices are smaller; 64 x 64 tiles do so for the smallest.  Measured: 4096 x 8192 x 8192 bf16 425 us = 1.29 PFLOP/s
-// (matrix cores busy 60 %), 512 x 8192 x 8192 in 8 bits 97 us = 0.71 PFLOP/s, weights from memory (34 %), 256 x 4096 x 4096 fp32 68 us
-// = 126 TFLOP/s (72 %).  Registers hold 256 x 256's sums and one k-tile under way: the early barrier's operands do not fit.
+// where the matrices are smaller; 64 x 64 tiles do so for the smallest.  Measured: 4096 x 8192 x 8192 bf16 428 us = 1.28 PFLOP/s
+// (matrix cores busy 59 %), 512 x 8192 x 8192 in 8 bits 96 us = 0.71 PFLOP/s, weights from memory (34 %), 256 x 4096 x 4096 fp32 68 us
+// = 127 TFLOP/s in a long run (72 %).  Registers hold 256 x 256's sums and one k-tile under way, just so: the instance for x in 8 bits
+// spills one, that of dx two, and the early barrier's operands do not fit.
 template <class C, int BM, int BN, int KS>
 constexpr int kLdsElems = KS * (BM + BN) * (kRowBytes / (int)sizeof(C));
 
@@ -644,9 +645,9 @@ __global__ __launch_bounds__(kFinishThreads) void k_join_all(const Join dx, unsi
 // ================================================================================================
 // One sample, or up to four: the product is the reading of w.  A wave takes two outputs and walks their rows of w, 512 q a
 // step, with the same q of x; a workgroup's outputs are whole chunks, or whole groups of 32 (WAVES = 16) where the results
-// are kept in 8 bits.  Bound by memory: all of a wave's requests for some thousand q are under way at once.  1 x 4096 x 4096
-// bf16: 7.3 us = 4.6 TB/s with the launch, against 14.1 with 64 x 64 tiles, split and joined.  Beyond four rows the
-// multiplications, 8 a row and value of w, would take longer than the reading.
+// are kept in 8 bits.  Bound by memory: all of a wave's requests for some thousand q are under way at once.  1, 2, 4 rows x 4096 x
+// 4096 bf16, with the launch: 7.9, 9.5, 10.9 us (one row in a long run 7.4 = 4.5 TB/s), against 12.8, 12.9, 12.9 with 64 x 64 tiles,
+// split and joined.  Beyond four rows the multiplications, 8 a row and value of w, would take longer than the reading.
 constexpr int kFewRows = 4, kFewOutputs = 2;
 template <class C, int XK, int ROWS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_few(const Args g) {
@@ -708,8 +709,10 @@ constexpr int kLeastTiles = 4;           // of the contraction a split has
 
 // The split of a product in tiles of one size that takes the least time: a turn of kGroups workgroups takes so many us for 1024 of the
 // contraction and so many for its start and end; splits store their sums and read them again at 5 TB/s, in a launch more.
-// Measured, us, 64 | 128 | 256, bf16 4096 x 4096 x 64: 19 | 20 | 17, x 512: 40 | 33 | 28, x 4096: 205 | 138 | 117; 2048 x 2048 x 64:
-// 6.7 | 8.5 | 14, x 1024: 18 | 15 | 30; 1024 x 2048 x 2048 17 | 25 | 37; 512 x 8192 x 8192 105 | 72 | 81, 4096 x 8192 x 8192 818 | 509 | 425.
+// Measured forward, us, 64 | 128 | 256, bf16 4096 x 4096 x 64: 19 | 20 | 17, x 512: 41 | 34 | 28, x 4096: 211 | 139 | 117; 2048 x 2048 x
+// 64: 7.2 | 8.4 | 14, x 1024: 19 | 17 | 31; 1024 x 2048 x 2048 18 | 20 | 29; 512 x 8192 x 8192 127 | 81 | 88, 4096 x 8192 x 8192 830 | 523 | 429.
+// The prices are these products'.  A backward pass of middle size takes more than they say, for its operands are read from LDS
+// transposed and its two products' turns are counted one by one: 2314 x 2020 x 632 bf16, both, 48 us where this says 29.
 Plan plan_with(int tile, int M, int N, int K, bool bf16) {
     const double start = tile == 64 ? 0.85 : tile == 128 ? 3.3 : 10.5;
     const double per_1024 = tile == 64 ? (bf16 ? 3.0 : 16.0) : tile == 128 ? 8.0 : 26.0;
@@ -781,9 +784,9 @@ hipError_t run(const Product& g, hipStream_t s) {
         return hipGetLastError();
     }
     // Where a compute unit has one workgroup, two groups of waves share its contraction, so that a matrix core's other wave
-    // multiplies while one waits, and divide the epilogue.  One group -> two, us: fp32 256 x 4096 x 4096 82 -> 75; bf16 256 x
-    // 4096 x 4096 19.7 -> 17.2, 768 x 4096 x 4096 36.7 -> 34.5, 512 x 8192 x 8192 in 8 bits 86.6 -> 79.  With more workgroups
-    // than that (fp32 1024 x 2048 x 2048: 66.6 -> 66.2) there is another wave anyway.
+    // multiplies while one waits, and divide the epilogue.  One group -> two, us, 60 passes at a time: fp32 256 x 4096 x 4096
+    // 80 -> 76; bf16 256 x 4096 x 4096 21.1 -> 19.9, 768 x 4096 x 4096 37.1 -> 35.9, 512 x 8192 x 8192 in 8 bits 103 -> 100.  With
+    // more workgroups than that there is another wave anyway.
     const bool alone = (long long)a.tiles_m * a.tiles_n * a.splits <= kGroups;
     if (p.bm == 256) {
         if constexpr (sizeof(C) == 2) start<C, PK, QK, PA, QA, 256, 256, 4, 2, 1, 1, false>(a, s);
