@@ -3,7 +3,8 @@ names, that marshals arguments and returns the lf_status; and objects that keep 
 `LeapfrogNet` keeps a net's.
 
 An object's outputs are overwritten by its next pass.  Work is enqueued on torch's current stream of the object's device, whatever
-the current device is.  A matrix in 8 bits may be loaded by several threads at once; any other object serves one at a time.
+the current device is.  A matrix in 8 bits may be loaded by several threads at once; any other object serves one thread and one
+stream at a time (its outputs and its workspace are the same in every pass).
 `rows` of an object is the most rows it takes: a call's inputs may have fewer, and its outputs then are views of the first ones."""
 from __future__ import annotations
 
