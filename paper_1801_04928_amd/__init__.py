@@ -15,11 +15,14 @@ from .binding import (  # noqa: F401
     LeapfrogNet,
 )
 from .operators import (  # noqa: F401
-    LF_MATRIX_F32, LF_MATRIX_BF16, LF_MATRIX_E4M3,
+    LF_MATRIX_F32, LF_MATRIX_BF16, LF_MATRIX_E4M3, LF_MATRIX_E4M3_128, LF_MATRIX_E4M3_TILES,
     LF_ACT_NONE, LF_ACT_SIGMOID, LF_ACT_RELU, LF_ACT_SILU, LF_ACT_GELU,
     lf_matrix, lf_checkpoint_save, lf_checkpoint_load, lf_norm_forward, lf_norm_workspace_bytes, lf_norm_backward,
     lf_linear_workspace_bytes, lf_linear_forward, lf_linear_backward_workspace_bytes, lf_linear_backward,
+    lf_layer_norm_forward, lf_layer_norm_workspace_bytes, lf_layer_norm_backward,
+    lf_block_save, lf_block_load, lf_block_linear_workspace_bytes, lf_block_linear_forward,
+    lf_block_linear_backward_workspace_bytes, lf_block_linear_backward, lf_distil,
     lf_operator_error,
-    E4M3Matrix, RmsNorm, Linear,
+    E4M3Matrix, E4M3Blocks, RmsNorm, LayerNorm, Linear, BlockLinear, Distillation,
 )
 from .residual_net import ResidualNet  # noqa: F401

@@ -1,0 +1,569 @@
+// The matrix product of operands in 8 bits with blocks of 128,  C[m][n] = sum_q P(m,q) Q(n,q)  with fp32 sums, both operands contiguous
+// along q: forward P = x, Q = w; for dx P = dz, Q = w^T; for dw P = dz^T, Q = x^T.
+//
+// Two ways to multiply.  Results in bf16 (or 8 bits): the instructions for 8 bits, which take the codes as they are and a scale byte
+// for each row's 32 q, all in one group here, so that 2^(byte - 127) costs nothing.  They add each eight consecutive products in 14
+// bits of the largest (smaller ones lose what lies below 2^-13 of it), and these sums in fp32: off by 2.4e-6 of the sum of the
+// products' magnitudes, root mean square, 2e-5 of a sum of random signs, a hundredth of what rounding to bf16 is off by and a
+// thousandth of what 8 bits do to the operands.  Results in fp32 (EXACT): the codes become bf16 numbers on their way from LDS, which is
+// exact, and the instructions for bf16 add exact products in fp32, at half the rate.
+#include "activation.h"
+#include "chunks.h"
+#include "column_sums.h"
+
+#include <algorithm>
+
+namespace lf {
+namespace ops {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+__host__ __device__ constexpr int ceil_div(int a, int b) { return a / b + (a % b != 0); }
+__host__ __device__ constexpr int whole_blocks(int cols) { return ceil_div(cols, kBlock) * kBlock; }
+
+struct Args {
+    Mat P, Q;
+    int M, N, K;
+    int tiles_m, tiles_n, k_tiles;        // k_tiles: of 128
+    int splits, k_tiles_per_split;
+    int p_shift, q_shift;                 // row >> shift is its row of scales
+    float* raw;                           // [splits][M][N] if splits > 1
+    Finish f;
+};
+
+// ---- what happens to finished sums -------------------------------------------------------------------------------------
+__device__ __forceinline__ void store_any(const Mat& m, long long row, int col, int n, const float (&v)[8], bool live) {
+    if (m.kind == E4M3_128) store_chunk<E4M3_128>(m, row, col, n, v, live);
+    else if (m.kind == F32) store_chunk<F32>(m, row, col, n, v, live);
+    else store_chunk<BF16>(m, row, col, n, v, live);
+}
+template <int ACT>
+__device__ __forceinline__ void activate_all(float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = activate(ACT, v[i]);
+}
+// Eight columns of row m from n on (n a multiple of 8; 16 neighbouring lanes hold the chunks of a group of 128).
+__device__ __forceinline__ void finish_chunk(const Finish& f, int M, int N, int m, int n, float (&v)[8], const float (&bias)[8]) {
+    const int there = m < M ? min(max(N - n, 0), kChunk) : 0;
+    const bool live = m < M && n < whole_blocks(N);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < there ? v[i] + bias[i] : 0.0f;
+    if (f.z.p) store_any(f.z, m, n, there, v, live);
+    switch (f.act) {                        // (the branch is outside the loop over the eight values)
+        case SIGMOID: activate_all<SIGMOID>(v); break;
+        case RELU: activate_all<RELU>(v); break;
+        case SILU: activate_all<SILU>(v); break;
+        case GELU: activate_all<GELU>(v); break;
+        default: break;
+    }
+    float residual[8] = {};
+    if (f.residual.p && there > 0) {
+        if (f.residual.kind == F32) load_values((const float*)f.residual.p + m * f.residual.ld + n, there, residual);
+        else load_values((const __bf16*)f.residual.p + m * f.residual.ld + n, there, residual);
+    }
+    // (past the row's end zeros: sigmoid(0) is not 0, and a group's scale looks at all of its values)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < there ? v[i] + residual[i] : 0.0f;
+    store_any(f.y, m, n, there, v, live);
+}
+__device__ __forceinline__ void load_bias(const Finish& f, int N, int n, float (&bias)[8]) {
+    if (f.bias) {
+        load_values(f.bias + n, min(max(N - n, 0), kChunk), bias);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+    }
+}
+
+// ================================================================================================
+// tiles of BM x BN by WM x WN waves
+// ================================================================================================
+// 64 lanes' 16 bytes each, from the buffer at voffset + soffset into LDS, lane after lane from `lds` on, past the registers.  (In
+// assembly, which has no output to be lost: the compiler, which does not know what in LDS a load is for, would wait for all
+// of them before any read of LDS.  The waits are next to the barriers.)
+__device__ __forceinline__ void load_to_lds(v4i resource, unsigned voffset, unsigned soffset, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(lds), "v"(voffset), "s"(resource), "s"(soffset)
+                 : "memory");
+}
+__device__ __forceinline__ void wait_and_meet() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ unsigned lds_address(const void* p) {
+    return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// A buffer of `bytes` from p on, both the same for the whole wave.
+__device__ __forceinline__ v4i resource_of(const uint8_t* p, unsigned bytes) {
+    const unsigned long long a = (unsigned long long)p;
+    return v4i{(int)__builtin_amdgcn_readfirstlane((unsigned)a), (int)(__builtin_amdgcn_readfirstlane((unsigned)(a >> 32)) & 0xffff),
+               (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000};
+}
+
+// The bf16 numbers that 32 codes stand for; the scale is the byte's in the lowest bits.
+__device__ __forceinline__ void values_of(const v8i& codes, int byte, v8bf (&v)[4]) {
+    const float scale = scale_power(byte & 255);          // (the instruction looks at the exponent alone)
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * h + w], scale, false);
+            const v2bf b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * h + w], scale, true);
+            v[h][4 * w] = a[0]; v[h][4 * w + 1] = a[1]; v[h][4 * w + 2] = b[0]; v[h][4 * w + 3] = b[1];
+        }
+}
+
+template <int BM, int BN, int WM, int WN>
+struct Shape {
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, MT = BM / WM / 32, NT = BN / WN / 32;
+    static constexpr int kStage = (BM + BN) * kBlock;                  // bytes of a k-tile of both operands
+    static constexpr int kPieces = (BM + BN) / 8 / kWaves;             // loads of a wave for it, 8 rows each
+    static constexpr int kPiecesM = BM / 8 / kWaves;
+    static constexpr int kFlatRows = WM * 16, kFlatLd = BN + 4;        // the epilogue's staging
+    static constexpr int kBytes = std::max(2 * kStage, 2 * kFlatRows * kFlatLd * 4);
+    static_assert(kPiecesM * 8 * kWaves == BM && kPieces * 8 * kWaves == BM + BN, "whole pieces for every wave");
+    static_assert((kWaves * 4) % 8 == 0, "the places of a lane's pieces are the same in all of its loads");
+};
+
+// A tile in LDS: rows of 128 bytes, eight pieces of 16, piece p of row i at place p ^ (i / 2 % 8), so that the pieces of 16 rows, which LDS
+// serves at once, lie in different banks.  The load to LDS puts lane after lane, so a lane asks for the piece that belongs to its
+// place.  Rows past the operand's last are the last again, which nothing looks at.
+template <int BM, int BN, int WM, int WN, bool EXACT>
+__device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint8_t* lds) {
+    typedef Shape<BM, BN, WM, WN> S;
+    constexpr int MT = S::MT, NT = S::NT, kWaves = S::kWaves, kThreads = S::kThreads;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r32 = lane & 31, half = lane >> 5;
+    // Workgroups are dealt to the 8 XCDs in turn: an XCD takes neighbouring tiles (and, of a split product, one split's) ...
+    const int tiles = g.tiles_m * g.tiles_n, total = tiles * g.splits;
+    const int per = total / 8, rest = total % 8, xcd = block % 8;
+    const int id = xcd * per + min(xcd, rest) + block / 8;
+    const int split = id / tiles, tile = id % tiles;
+    // ... in bands of eight rows of tiles
+    const int band = tile / (8 * g.tiles_n), high = min(8, g.tiles_m - 8 * band), in_band = tile - 8 * band * g.tiles_n;
+    const int m0 = (8 * band + in_band % high) * BM, n0 = in_band / high * BN;
+    const int wm = wave / WN * (MT * 32), wn = wave % WN * (NT * 32);
+    const int kt0 = split * g.k_tiles_per_split, turns = min(g.k_tiles, kt0 + g.k_tiles_per_split) - kt0;
+
+    v16f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+    if (turns > 0) {
+        const unsigned ld_p = (unsigned)g.P.ld, ld_q = (unsigned)g.Q.ld, last_p = min(BM, g.M - m0) - 1, last_q = min(BN, g.N - n0) - 1;
+        const unsigned row_bytes = (unsigned)whole_blocks(g.K);
+        const v4i res_p = resource_of((const uint8_t*)g.P.p + (long long)m0 * g.P.ld, last_p * ld_p + row_bytes);
+        const v4i res_q = resource_of((const uint8_t*)g.Q.p + (long long)n0 * g.Q.ld, last_q * ld_q + row_bytes);
+        const unsigned base = lds_address(lds), row_in = wave * 8 + lane / 8;
+        const unsigned piece = ((lane & 7) ^ ((row_in >> 1) & 7)) * 16;
+        const unsigned first_p = row_in * ld_p, first_q = row_in * ld_q;
+        auto request = [&](int turn, unsigned buffer) {
+            const unsigned k = (unsigned)(kt0 + turn) * kBlock;
+#pragma unroll
+            for (int u = 0; u < S::kPieces; ++u) {
+                const bool p = u < S::kPiecesM;
+                const unsigned v = p ? min(first_p + u * kWaves * 8 * ld_p, last_p * ld_p) : min(first_q + (u - S::kPiecesM) * kWaves * 8 * ld_q, last_q * ld_q);
+                load_to_lds(p ? res_p : res_q, v + piece, k, base + buffer + (u * kWaves + wave) * 1024);
+            }
+        };
+        // codes past the contraction's end become zeros (in the last k-tile)
+        const int tail = g.K - (g.k_tiles - 1) * kBlock;
+        auto mend = [&](int turn, unsigned buffer) {
+            if (tail == kBlock || kt0 + turn != g.k_tiles - 1) return;
+            for (int i = t; i < (BM + BN) * 8; i += kThreads) {
+                const int row = i / 8, p = i % 8;
+                v4u* at = reinterpret_cast<v4u*>(lds + buffer + row * kBlock + ((p ^ (row >> 1)) & 7) * 16);
+                if (p * 16 + 16 > tail) {
+                    v4u v = *at;
+                    keep_codes(v, tail - p * 16);
+                    *at = v;
+                }
+            }
+            wait_and_meet();
+        };
+        // scales: four k-tiles' in a register, the next four's under way
+        const uint8_t* scales_p[MT];
+        const uint8_t* scales_q[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) scales_p[i] = g.P.scales + (long long)(min(m0 + wm + 32 * i + r32, g.M - 1) >> g.p_shift) * g.P.scale_ld;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) scales_q[j] = g.Q.scales + (long long)(min(n0 + wn + 32 * j + r32, g.N - 1) >> g.q_shift) * g.Q.scale_ld;
+        int four_p[MT], four_q[NT];
+        auto scales = [&](int turn) {
+            const int at = (kt0 + turn) & ~3;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) four_p[i] = *as_global<const int>(scales_p[i] + at);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) four_q[j] = *as_global<const int>(scales_q[j] + at);
+        };
+        // an operand of one step, 64 q: lane holds 32 q of row r32, pieces 4 step + 2 half and the next
+        const unsigned turn_p = ((r32 >> 1) & 7), at_p = (wm + r32) * kBlock, at_q = (BM + wn + r32) * kBlock;
+        v8i a[2][MT], q[2][NT];
+        auto read = [&](int step, unsigned buffer, v8i (&fa)[MT], v8i (&fq)[NT]) {
+            const unsigned lo = ((4 * step + 2 * half) ^ turn_p) * 16, hi = lo ^ 16;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const v4i x = *reinterpret_cast<const v4i*>(lds + buffer + at_p + lo + 32 * i * kBlock);
+                const v4i y = *reinterpret_cast<const v4i*>(lds + buffer + at_p + hi + 32 * i * kBlock);
+                fa[i] = v8i{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const v4i x = *reinterpret_cast<const v4i*>(lds + buffer + at_q + lo + 32 * j * kBlock);
+                const v4i y = *reinterpret_cast<const v4i*>(lds + buffer + at_q + hi + 32 * j * kBlock);
+                fq[j] = v8i{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            }
+        };
+        int sp[MT], sq[NT];
+        auto multiply = [&](const v8i (&fa)[MT], const v8i (&fq)[NT]) {
+            if constexpr (EXACT) {
+                v8bf x[MT][4];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) values_of(fa[i], sp[i], x[i]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    v8bf y[4];
+                    values_of(fq[j], sq[j], y);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][h], y[h], acc[i][j], 0, 0, 0);
+                }
+                return;
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fq[j], acc[i][j], 0, 0, 0, sp[i], 0, sq[j]);
+        };
+        auto shift = [&](int turn) {
+            const int by = ((kt0 + turn) & 3) * 8;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sp[i] = four_p[i] >> by;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sq[j] = four_q[j] >> by;
+        };
+        // A k-tile is in LDS, the next on its way to the other half of it.  The barrier stands between a k-tile's two steps: by then
+        // every wave has the second step's operands in registers, the half is free for the k-tile after the next, and the next
+        // k-tile's first operands are read while the second step is multiplied.
+        scales(0);
+        request(0, 0);
+        wait_and_meet();
+        mend(0, 0);
+        if (turns > 1) request(1, S::kStage);
+        read(0, 0, a[0], q[0]);
+        unsigned buffer = 0;
+        for (int turn = 0; turn < turns; ++turn) {
+            shift(turn);
+            read(1, buffer, a[1], q[1]);
+            multiply(a[0], q[0]);
+            wait_and_meet();
+            mend(turn + 1, buffer ^ S::kStage);
+            if (((kt0 + turn + 1) & 3) == 0) scales(turn + 1);
+            if (turn + 2 < turns) request(turn + 2, buffer);
+            read(0, buffer ^ S::kStage, a[0], q[0]);
+            multiply(a[1], q[1]);
+            buffer ^= S::kStage;
+        }
+        __syncthreads();          // LDS becomes the epilogue's
+    }
+
+    // Accumulator element e of lane (r32, half) of square (i, j) is C[.. 32 i + 8 (e / 4) + 4 half + e % 4][.. 32 j + r32].  Rows turn through LDS, 16 of
+    // every wave's at a time, so that 16 lanes hold 128 consecutive columns; the two halves of LDS take turns.
+    float* const flat = reinterpret_cast<float*>(lds);
+    constexpr int kAcross = BN / kChunk, kDown = kThreads / kAcross;
+    const int across = t % kAcross, n = n0 + across * kChunk;
+    float bias[8];
+    load_bias(g.f, g.splits == 1 ? g.N : 0, n, bias);
+#pragma unroll
+    for (int u = 0; u < 2 * MT; ++u) {
+        float* const stage = flat + (u & 1) * S::kFlatRows * S::kFlatLd;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                stage[(wave / WN * 16 + 8 * (e >> 2) + 4 * half + (e & 3)) * S::kFlatLd + wn + 32 * j + r32] = acc[u / 2][j][(u & 1) * 8 + e];
+        __syncthreads();
+#pragma unroll 1
+        for (int row = t / kAcross; row < S::kFlatRows; row += kDown) {
+            const int m = m0 + row / 16 * (MT * 32) + u * 16 + row % 16;
+            const v4f lo = *reinterpret_cast<const v4f*>(stage + row * S::kFlatLd + across * kChunk);
+            const v4f hi = *reinterpret_cast<const v4f*>(stage + row * S::kFlatLd + across * kChunk + 4);
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (g.splits > 1) {
+                if (m < g.M && n < g.N) store_values(g.raw + ((size_t)split * g.M + m) * g.N + n, min(g.N - n, kChunk), v);
+            } else {
+                finish_chunk(g.f, g.M, g.N, m, n, v, bias);
+            }
+        }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, bool EXACT>
+__global__ __launch_bounds__(64 * WM * WN) void k_block_product(const Args g) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[Shape<BM, BN, WM, WN>::kBytes];
+    product_tile<BM, BN, WM, WN, EXACT>(g, blockIdx.x, lds);
+}
+
+// Sums of the splits' partial sums, in their order, and what follows.
+struct Join {
+    const float* raw;
+    int splits, M, N, chunks;
+    Finish f;
+};
+Join join_of(const Args& a) { return Join{a.raw, a.splits, a.M, a.N, whole_blocks(a.N) / kChunk, a.f}; }
+unsigned join_blocks(const Join& a, int threads) {
+    return a.splits > 1 ? (unsigned)(((long long)a.M * a.chunks + threads - 1) / threads) : 0;
+}
+template <int THREADS>
+__device__ __forceinline__ void join(const Join& a, unsigned block) {
+    const long long id = (long long)block * THREADS + threadIdx.x;
+    const long long row = id / a.chunks;
+    const int n = (int)(id % a.chunks) * kChunk;
+    const int m = row < a.M ? (int)row : a.M;                 // lanes past the end stay with their group
+    const int there = m < a.M ? min(max(a.N - n, 0), kChunk) : 0;
+    float v[8] = {}, bias[8];
+    load_bias(a.f, a.N, n, bias);
+    const float* at = a.raw + (size_t)m * a.N + n;
+    const size_t step = (size_t)a.M * a.N;
+    if (there > 0) {
+#pragma unroll 4
+        for (int p = 0; p < a.splits; ++p) {
+            float u[8];
+            load_values(at + p * step, there, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += u[i];
+        }
+    }
+    finish_chunk(a.f, a.M, a.N, m, n, v, bias);
+}
+// What split products end with, in one launch: the sums of up to two, and those of db.
+__global__ __launch_bounds__(kFinishThreads) void k_block_join(const Join x, unsigned x_blocks, const Join w, unsigned w_blocks, const ColumnSums db) {
+    if (blockIdx.x < x_blocks) join<kFinishThreads>(x, blockIdx.x);
+    else if (blockIdx.x < x_blocks + w_blocks) join<kFinishThreads>(w, blockIdx.x - x_blocks);
+    else finish_columns(db, blockIdx.x - x_blocks - w_blocks);
+}
+
+// ================================================================================================
+// a few rows
+// ================================================================================================
+// Up to 16 MT rows: the product is the reading of Q.  A workgroup takes 16 outputs, each of its waves every kFewWaves-th group of 128 of the
+// contraction: a lane has 2 x 16 bytes of its output's row (and of its sample's), which the matrix instruction takes as they come, for
+// operands of one order of q on both sides.  P may be dense: its group is put into 8 bits in registers, the four lanes that
+// hold a row's group finding its scale.
+constexpr int kFewWaves = 8, kFewOutputs = 16;
+template <int XK>
+__device__ __forceinline__ v8i few_operand(const Mat& m, long long row, int k, int half16, int there, int& byte) {
+    if constexpr (XK == E4M3_128) {
+        const uint8_t* p = (const uint8_t*)m.p + row * m.ld + (long long)k * kBlock + half16 * 16;
+        v4u x = *as_global<const v4u>(p), y = *as_global<const v4u>(p + 64);
+        byte = *as_global<const uint8_t>(m.scales + row * m.scale_ld + k);
+        if (there < kBlock) {
+            keep_codes(x, there - half16 * 16);
+            keep_codes(y, there - 64 - half16 * 16);
+        }
+        return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+    } else {
+        typedef typename Stored<XK>::type T;
+        float v[4][8];
+        const T* p = (const T*)m.p + row * m.ld + (long long)k * kBlock;
+        unsigned top = 0;
+        bool odd = false;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int col = h / 2 * 64 + half16 * 16 + h % 2 * 8;
+            load_values(p + col, min(max(there - col, 0), kChunk), v[h]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const unsigned b = __float_as_uint(finite_magnitude(v[h][i]));
+                odd |= !(fabsf(v[h][i]) < __builtin_inff());
+                top = max(top, b);
+            }
+        }
+        top = max(top, (unsigned)__shfl_xor((int)top, 16));
+        top = max(top, (unsigned)__shfl_xor((int)top, 32));
+        byte = scale_byte(__uint_as_float(top));
+        const float inverse = scale_power(254 - byte), most = byte == kLargestScale ? 240.0f : 448.0f;
+        v8i out;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            float s[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[i] = fminf(fmaxf(v[h][i] * inverse, -most), most);
+                if (odd) s[i] = fabsf(v[h][i]) < __builtin_inff() ? s[i] : __builtin_nanf("");
+            }
+            const v2u w = convert_eight(s);
+            out[2 * h] = (int)w[0];
+            out[2 * h + 1] = (int)w[1];
+        }
+        return out;
+    }
+}
+
+template <int XK, int MT, bool EXACT>
+__global__ __launch_bounds__(64 * kFewWaves) void k_block_few(const Args g) {
+    __shared__ float sums[kFewWaves][16 * MT][kFewOutputs + 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, quarter = lane >> 4;
+    const int n0 = blockIdx.x * kFewOutputs, n = min(n0 + r16, g.N - 1);
+    v4f acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint8_t* q_row = (const uint8_t*)g.Q.p + (long long)n * g.Q.ld + quarter * 16;
+    const uint8_t* q_scales = g.Q.scales + (long long)(n >> g.q_shift) * g.Q.scale_ld;
+    const auto group = [&](int k) {
+        const int there = min(g.K - k * kBlock, kBlock);
+        v4u x = *as_global<const v4u>(q_row + (long long)k * kBlock), y = *as_global<const v4u>(q_row + (long long)k * kBlock + 64);
+        const int q_byte = *as_global<const uint8_t>(q_scales + k);
+        if (there < kBlock) {
+            keep_codes(x, there - quarter * 16);
+            keep_codes(y, there - 64 - quarter * 16);
+        }
+        const v8i b = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        v8bf values[4];
+        if constexpr (EXACT) values_of(b, q_byte, values);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            int byte;
+            const v8i a = few_operand<XK>(g.P, min(16 * i + r16, g.M - 1), k, quarter, there, byte);
+            if constexpr (EXACT) {
+                v8bf x[4];
+                values_of(a, byte, x);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[h], values[h], acc[i], 0, 0, 0);
+            } else {
+                acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[i], 0, 0, 0, byte, 0, q_byte);
+            }
+        }
+    };
+    int k = wave;
+    for (; k + 3 * kFewWaves < g.k_tiles; k += 4 * kFewWaves) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) group(k + u * kFewWaves);
+    }
+    for (; k < g.k_tiles; k += kFewWaves) group(k);
+    // element e of lane (r16, quarter): row 4 quarter + e, output r16
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[wave][16 * i + 4 * quarter + e][r16] = acc[i][e];
+    __syncthreads();
+    constexpr int kChunks = kFewOutputs / kChunk;
+    if (threadIdx.x >= 16 * MT * kChunks) return;
+    const int m = threadIdx.x / kChunks, col = threadIdx.x % kChunks * kChunk;
+    if (m >= g.M || n0 + col >= g.N) return;
+    float v[8] = {}, bias[8];
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += sums[w][m][col + i];
+    load_bias(g.f, g.N, n0 + col, bias);
+    finish_chunk(g.f, g.M, g.N, m, n0 + col, v, bias);
+}
+constexpr int kFewRows = 64, kDenseRows = 16;
+bool eight(const Mat& m) { return m.kind == E4M3_128; }      // (that a result is there is not needed for this)
+bool few_outputs(const Mat& y, const Mat& z) { return !eight(y) && !(z.p && eight(z)); }
+
+// ---- which tiles ---------------------------------------------------------------------------------------------------------
+struct Plan {
+    int tile, splits, k_tiles_per_split;
+    double us;                           // what it takes, by the measurements
+};
+constexpr int kGroups = 256;             // workgroups that fill the chip
+constexpr int kLeastTiles = 2;           // of the contraction a split has
+
+Plan plan_with(int tile, int M, int N, int K) {
+    const double start = tile == 128 ? 3.3 : 8.0, per_1024 = tile == 128 ? 4.0 : 13.0;
+    const int k_tiles = ceil_div(K, kBlock);
+    const long long tiles = (long long)ceil_div(M, tile) * ceil_div(N, tile);
+    const int most = (int)std::max<long long>(1, std::min<long long>(kGroups / tiles, k_tiles / kLeastTiles));
+    Plan best{tile, 1, k_tiles, 1e300};
+    for (int want = 1; want <= most; want = want < most && 2 * want > most ? most : 2 * want) {
+        const int per = std::max(1, ceil_div(k_tiles, want)), splits = std::max(1, ceil_div(k_tiles, per));
+        double us = (double)((tiles * splits + kGroups - 1) / kGroups) * (start + per_1024 * per * kBlock / 1024);
+        if (splits > 1) us += 3.0 + (double)splits * M * N * 8 / 5e6;
+        if (us < best.us) best = Plan{tile, splits, per, us};
+    }
+    return best;
+}
+Plan plan_of(int M, int N, int K) {
+    const Plan small = plan_with(128, M, N, K), large = plan_with(256, M, N, K);
+    return large.us < small.us ? large : small;
+}
+
+Args args_of(const BlockProduct& g, const Plan& p) {
+    return Args{g.P, g.Q, g.M, g.N, g.K, ceil_div(g.M, p.tile), ceil_div(g.N, p.tile), ceil_div(g.K, kBlock), p.splits, p.k_tiles_per_split,
+                g.P.kind == E4M3_TILES ? 7 : 0, g.Q.kind == E4M3_TILES ? 7 : 0, g.raw, g.f};
+}
+const ColumnSums kNoSums{nullptr, 0, 0, nullptr};
+const Join kNoJoin{nullptr, 1, 0, 0, 0, Finish{}};
+
+template <int XK, bool EXACT>
+void few(const Args& a, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div(a.N, kFewOutputs));
+    if (a.M <= 16) k_block_few<XK, 1, EXACT><<<grid, 64 * kFewWaves, 0, s>>>(a);
+    else if constexpr (XK == E4M3_128) {
+        if (a.M <= 32) k_block_few<XK, 2, EXACT><<<grid, 64 * kFewWaves, 0, s>>>(a);
+        else k_block_few<XK, 4, EXACT><<<grid, 64 * kFewWaves, 0, s>>>(a);
+    }
+}
+// Whether a result shows what the instructions for 8 bits lose.
+bool exact(const Finish& f) { return f.y.kind == F32 || (f.z.p && f.z.kind == F32); }
+hipError_t finish(const Join& x, const Join& w, const ColumnSums& db, hipStream_t s) {
+    const unsigned bx = join_blocks(x, kFinishThreads), bw = join_blocks(w, kFinishThreads), bb = finish_blocks(db);
+    if (bx + bw + bb == 0) return hipSuccess;
+    k_block_join<<<dim3(bx + bw + bb), kFinishThreads, 0, s>>>(x, bx, w, bw, db);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Of any plan of this product and of smaller ones: splits <= k_tiles / kLeastTiles, and splits * tiles <= kGroups.
+size_t block_product_scratch_bytes(int M, int N, int K) {
+    const int splits = ceil_div(K, kBlock) / kLeastTiles;
+    if (splits < 2) return 0;
+    return std::min((size_t)kGroups * 256 * 256, (size_t)splits * M * N) * sizeof(float);
+}
+
+bool block_product_takes_dense(int M, const Mat& y, const Mat& z) { return M <= kDenseRows && few_outputs(y, z); }
+
+hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
+    if (g.M <= kFewRows && few_outputs(g.f.y, g.f.z) && g.P.kind != E4M3_TILES) {
+        const Args a = args_of(g, Plan{128, 1, 1, 0});
+        if (g.P.kind == F32) few<F32, true>(a, s);             // (results have the storage type of a dense P)
+        else if (g.P.kind == BF16) few<BF16, false>(a, s);
+        else if (exact(g.f)) few<E4M3_128, true>(a, s);
+        else few<E4M3_128, false>(a, s);
+        return hipGetLastError();
+    }
+    const Plan p = plan_of(g.M, g.N, g.K);
+    const Args a = args_of(g, p);
+    const dim3 grid((unsigned)a.tiles_m * a.tiles_n * a.splits);
+    if (exact(g.f)) {
+        if (p.tile == 256) k_block_product<256, 256, 4, 2, true><<<grid, 512, 0, s>>>(a);
+        else k_block_product<128, 128, 2, 2, true><<<grid, 256, 0, s>>>(a);
+    } else {
+        if (p.tile == 256) k_block_product<256, 256, 4, 2, false><<<grid, 512, 0, s>>>(a);
+        else k_block_product<128, 128, 2, 2, false><<<grid, 256, 0, s>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : finish(join_of(a), kNoJoin, kNoSums, s);
+}
+
+hipError_t launch_block_backward(const BlockProduct& dx, const BlockProduct& dw, const ColumnSums& db, hipStream_t s) {
+    hipError_t e = finish(kNoJoin, kNoJoin, db, s);
+    if (e == hipSuccess && dx.f.y.p && dx.M > 0) e = launch_block_product(dx, s);
+    if (e == hipSuccess && dw.f.y.p) e = launch_block_product(dw, s);
+    return e;
+}
+
+}  // namespace ops
+}  // namespace lf

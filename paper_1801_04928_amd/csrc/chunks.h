@@ -8,6 +8,7 @@ namespace lf {
 namespace ops {
 
 constexpr int kGroup = 32;        // values that share a scale
+constexpr int kBlock = 128;       // the same, in blocks of 128
 constexpr int kChunk = 8;
 
 typedef unsigned int v2u __attribute__((ext_vector_type(2)));
@@ -92,6 +93,15 @@ __device__ __forceinline__ unsigned quad_max(unsigned m) {
     m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));
     return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));
 }
+// Largest of the 16 lanes of a row of lanes (all of them active).
+__device__ __forceinline__ unsigned sixteen_max(unsigned m) {
+    m = quad_max(m);
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x124, 0xF, 0xF, true));
+    return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x128, 0xF, 0xF, true));
+}
+// Largest among the lanes that hold a group's chunks, four of 32 columns or sixteen of 128.
+template <int KIND> __device__ __forceinline__ unsigned group_max(unsigned m) { return KIND == E4M3 ? quad_max(m) : sixteen_max(m); }
+template <int KIND> constexpr int kGroupOf = KIND == E4M3 ? kGroup : kBlock;
 __device__ __forceinline__ v2u convert_eight(const float (&v)[8]) {
     int w[2];
 #pragma unroll
@@ -105,11 +115,12 @@ constexpr int kLargestScale = 247;          // of the largest finite numbers
 // Codes (rounded to nearest even) and scale of a group's chunk.  The largest of the values' bits without their signs tells what
 // the group holds: with every value finite and a scale below the largest no product with the scale's reciprocal passes
 // 448 and there is nothing to look at value by value, which would take twice the instructions.
+template <int KIND = E4M3>
 __device__ __forceinline__ v2u eight_codes(const float (&v)[8], int& byte) {
     unsigned top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    byte = scale_byte(__uint_as_float(quad_max(top)));
+    byte = scale_byte(__uint_as_float(group_max<KIND>(top)));
     float s[8];
     if (byte < kLargestScale) {
         const float inverse = scale_power(254 - byte);
@@ -119,7 +130,7 @@ __device__ __forceinline__ v2u eight_codes(const float (&v)[8], int& byte) {
         unsigned finite = 0;                  // NaN and infinities do not set a scale
 #pragma unroll
         for (int i = 0; i < 8; ++i) finite = max(finite, __float_as_uint(finite_magnitude(v[i])));
-        byte = scale_byte(__uint_as_float(quad_max(finite)));
+        byte = scale_byte(__uint_as_float(group_max<KIND>(finite)));
         const float inverse = scale_power(254 - byte);
         const float most = byte == kLargestScale ? 240.0f : 448.0f;      // 256 * 2^120 would be no finite number
 #pragma unroll
@@ -130,14 +141,15 @@ __device__ __forceinline__ v2u eight_codes(const float (&v)[8], int& byte) {
     }
     return convert_eight(s);
 }
-// Chunk `col` (a multiple of 8) of a row in 8 bits.  The four lanes of a quad hold the four chunks of a group and all call this;
-// values past the last column are zero.  live: the chunk's group begins inside the row, so its memory is there.
+// Chunk `col` (a multiple of 8) of a row in 8 bits.  Neighbouring lanes (four, or sixteen of blocks of 128) hold the chunks of a group and
+// all call this; values past the last column are zero.  live: the chunk's group begins inside the row, so its memory is there.
+template <int KIND = E4M3>
 __device__ __forceinline__ void store_eight(uint8_t* codes, uint8_t* scales, int col, const float (&v)[8], bool live) {
     int byte;
-    const v2u w = eight_codes(v, byte);
+    const v2u w = eight_codes<KIND>(v, byte);
     if (live) {
         *as_global<v2u>(codes + col) = w;
-        if (col % kGroup == 0) *as_global<uint8_t>(scales + col / kGroup) = (uint8_t)byte;
+        if (col % kGroupOf<KIND> == 0) *as_global<uint8_t>(scales + col / kGroupOf<KIND>) = (uint8_t)byte;
     }
 }
 // The values of eight codes.
@@ -246,10 +258,11 @@ __device__ __forceinline__ void take_chunk(Chunk<KIND> c, int n, float (&v)[8]) 
 // Values col .. col + n - 1 of a row (n <= 8; n <= 0: none), the others zero; col is a multiple of 8.
 template <int KIND>
 __device__ __forceinline__ void load_chunk(const Mat& m, long long row, int col, int n, float (&v)[8]) {
-    if constexpr (KIND == E4M3) {
+    if constexpr (KIND >= E4M3) {
         if (n > 0) {
             const v2u w = *as_global<const v2u>((const uint8_t*)m.p + row * m.ld + col);
-            eight_values(w, scale_value(*as_global<const uint8_t>(m.scales + row * m.scale_ld + col / kGroup)), v);
+            const long long scale_row = KIND == E4M3_TILES ? row / kBlock : row;
+            eight_values(w, scale_value(*as_global<const uint8_t>(m.scales + scale_row * m.scale_ld + col / kGroupOf<KIND>)), v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.0f;
         } else {
@@ -264,8 +277,8 @@ __device__ __forceinline__ void load_chunk(const Mat& m, long long row, int col,
 // All lanes call this (see store_eight); live: the row is there and col < the row's columns rounded up to whole groups.
 template <int KIND>
 __device__ __forceinline__ void store_chunk(const Mat& m, long long row, int col, int n, const float (&v)[8], bool live) {
-    if constexpr (KIND == E4M3) {
-        store_eight((uint8_t*)m.p + row * m.ld, m.scales + row * m.scale_ld, col, v, live);
+    if constexpr (KIND == E4M3 || KIND == E4M3_128) {
+        store_eight<KIND>((uint8_t*)m.p + row * m.ld, m.scales + row * m.scale_ld, col, v, live);
     } else {
         typedef typename Stored<KIND>::type T;
         if (live && n > 0) store_values((T*)m.p + row * m.ld + col, n, v);

@@ -8,7 +8,7 @@
 namespace lf {
 namespace ops {
 
-enum Kind { F32 = 0, BF16 = 1, E4M3 = 2 };      // lf_matrix_type
+enum Kind { F32 = 0, BF16 = 1, E4M3 = 2, E4M3_128 = 3, E4M3_TILES = 4 };      // lf_matrix_type
 
 // A matrix as kernels take it.  p == nullptr: not there.
 struct Mat {
@@ -64,6 +64,55 @@ size_t product_scratch_bytes(int M, int N, int K, bool bf16);
 hipError_t launch_product(const Product& g, hipStream_t s);
 // The two products of a backward pass, each with scratch of its own, and what is left to do for db.
 hipError_t launch_backward(const Product& dx, const Product& dw, const ColumnSums& db, hipStream_t s);
+
+// ---- layer_norm_kernels.hip ------------------------------------------------------------------------------------------
+hipError_t launch_layer_norm_forward(int rows, int cols, const Mat& x, const Mat& branch, const float* gain, const float* shift,
+                                     float eps, const Mat& sum, const Mat& y, float* mean, float* rstd, hipStream_t s);
+// partial: [layer_norm_partials(rows, cols)][2][cols] fp32, needed with dgain or dshift
+int layer_norm_partials(int rows, int cols);
+hipError_t launch_layer_norm_backward(int rows, int cols, const Mat& dy, const Mat& sum, const float* gain, const float* mean,
+                                      const float* rstd, const Mat& dsum, const Mat& dx, float* dgain, float* dshift,
+                                      float* partial, hipStream_t s);
+
+// ---- block_kernels.hip ---------------------------------------------------------------------------------------------
+// d = x act'(z), or x (z absent), into 8 bits with blocks of 128 as it lies (out) and transposed (out_t), either may be absent; and
+// sums over each 128 of its rows into partial ([block_partials(rows)][cols], may be null)
+struct BlockSave {
+    int rows, cols, act;
+    Mat x, z, out, out_t;
+    float* partial;
+};
+int block_partials(int rows);
+hipError_t launch_block_save(const BlockSave& a, hipStream_t s);
+hipError_t launch_block_load(int rows, int cols, const Mat& in, const Mat& out, hipStream_t s);
+
+// ---- block_product_kernels.hip -----------------------------------------------------------------------------------------
+// C[m][n] = sum_q P(m,q) Q(n,q), both contiguous along q in 8 bits with blocks of 128; P may be dense for the products of a few rows
+// (block_product_takes_dense).  raw: fp32 scratch, block_product_scratch_bytes(...) of it.
+struct BlockProduct {
+    Mat P, Q;
+    int M, N, K;
+    Finish f;
+    float* raw;
+};
+size_t block_product_scratch_bytes(int M, int N, int K);
+bool block_product_takes_dense(int M, const Mat& y, const Mat& z);
+hipError_t launch_block_product(const BlockProduct& g, hipStream_t s);
+// The two products of a backward pass, each with scratch of its own.
+hipError_t launch_block_backward(const BlockProduct& dx, const BlockProduct& dw, const ColumnSums& db, hipStream_t s);
+
+// ---- distil_kernels.hip --------------------------------------------------------------------------------------------
+constexpr int kMostTop = 1024;
+struct Distil {
+    int rows, classes, top;
+    Mat logits, top_logits, dlogits;
+    const int* top_classes;
+    long long top_classes_ld;
+    float temperature;
+    const float* weight;
+    float* loss;
+};
+hipError_t launch_distil(const Distil& a, hipStream_t s);
 
 }  // namespace ops
 }  // namespace lf

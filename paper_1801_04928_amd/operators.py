@@ -13,11 +13,12 @@ from typing import Optional
 
 from .binding import LF_BF16, LF_EINVAL, LF_F32, LF_OK, LfError, lib
 
-LF_MATRIX_F32, LF_MATRIX_BF16, LF_MATRIX_E4M3 = range(3)
+LF_MATRIX_F32, LF_MATRIX_BF16, LF_MATRIX_E4M3, LF_MATRIX_E4M3_128, LF_MATRIX_E4M3_TILES = range(5)
 LF_ACT_NONE, LF_ACT_SIGMOID, LF_ACT_RELU, LF_ACT_SILU, LF_ACT_GELU = range(5)
 ACTIVATIONS = {"none": LF_ACT_NONE, "sigmoid": LF_ACT_SIGMOID, "relu": LF_ACT_RELU, "silu": LF_ACT_SILU,
                "gelu": LF_ACT_GELU}
 GROUP = 32          # values of a row that share a scale in 8 bits
+BLOCK = 128         # the same, in blocks of 128
 
 
 class lf_matrix(C.Structure):
@@ -44,6 +45,16 @@ def _lib() -> C.CDLL:
                 ("lf_linear_forward", i, [i, i, i, mp, mp, vp, i, mp, mp, mp, vp, sz, vp]),
                 ("lf_linear_backward_workspace_bytes", sz, [i, i, i, i]),
                 ("lf_linear_backward", i, [i, i, i, mp, mp, i, mp, mp, mp, mp, vp, vp, sz, vp]),
+                ("lf_layer_norm_forward", i, [i, i, mp, mp, vp, vp, f, mp, mp, vp, vp, vp]),
+                ("lf_layer_norm_workspace_bytes", sz, [i, i]),
+                ("lf_layer_norm_backward", i, [i, i, mp, mp, vp, vp, vp, mp, mp, vp, vp, vp, sz, vp]),
+                ("lf_block_save", i, [i, i, mp, mp, mp, vp]),
+                ("lf_block_load", i, [i, i, mp, mp, vp]),
+                ("lf_block_linear_workspace_bytes", sz, [i, i, i]),
+                ("lf_block_linear_forward", i, [i, i, i, mp, mp, vp, i, mp, mp, mp, mp, vp, sz, vp]),
+                ("lf_block_linear_backward_workspace_bytes", sz, [i, i, i]),
+                ("lf_block_linear_backward", i, [i, i, i, mp, mp, i, mp, mp, mp, mp, vp, vp, sz, vp]),
+                ("lf_distil", i, [i, i, i, mp, mp, vp, C.c_longlong, f, vp, vp, mp, vp]),
                 ("lf_operator_error", C.c_char_p, [])]:
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
@@ -91,6 +102,54 @@ def lf_linear_backward(rows, outputs, inputs, dy, z, act, x, w, dx, dw, db, work
                        hip_stream=0) -> int:
     return _lib().lf_linear_backward(rows, outputs, inputs, dy, z, act, x, w, dx, dw, db, workspace, workspace_bytes,
                                      hip_stream)
+
+
+def lf_layer_norm_forward(rows, cols, x, branch, gain, shift, eps, sum_, y, mean, rstd, hip_stream=0) -> int:
+    return _lib().lf_layer_norm_forward(rows, cols, x, branch, gain, shift, eps, sum_, y, mean, rstd, hip_stream)
+
+
+def lf_layer_norm_workspace_bytes(rows, cols) -> int:
+    return _lib().lf_layer_norm_workspace_bytes(rows, cols)
+
+
+def lf_layer_norm_backward(rows, cols, dy, sum_, gain, mean, rstd, dsum, dx, dgain, dshift, workspace, workspace_bytes,
+                           hip_stream=0) -> int:
+    return _lib().lf_layer_norm_backward(rows, cols, dy, sum_, gain, mean, rstd, dsum, dx, dgain, dshift, workspace,
+                                         workspace_bytes, hip_stream)
+
+
+def lf_block_save(rows, cols, x, out, out_t, hip_stream=0) -> int:
+    return _lib().lf_block_save(rows, cols, x, out, out_t, hip_stream)
+
+
+def lf_block_load(rows, cols, in_, out, hip_stream=0) -> int:
+    return _lib().lf_block_load(rows, cols, in_, out, hip_stream)
+
+
+def lf_block_linear_workspace_bytes(rows, outputs, inputs) -> int:
+    return _lib().lf_block_linear_workspace_bytes(rows, outputs, inputs)
+
+
+def lf_block_linear_forward(rows, outputs, inputs, x, w, bias, act, residual, y, z, x_t, workspace, workspace_bytes,
+                            hip_stream=0) -> int:
+    return _lib().lf_block_linear_forward(rows, outputs, inputs, x, w, bias, act, residual, y, z, x_t, workspace,
+                                          workspace_bytes, hip_stream)
+
+
+def lf_block_linear_backward_workspace_bytes(rows, outputs, inputs) -> int:
+    return _lib().lf_block_linear_backward_workspace_bytes(rows, outputs, inputs)
+
+
+def lf_block_linear_backward(rows, outputs, inputs, dy, z, act, x_t, w_t, dx, dw, db, workspace, workspace_bytes,
+                             hip_stream=0) -> int:
+    return _lib().lf_block_linear_backward(rows, outputs, inputs, dy, z, act, x_t, w_t, dx, dw, db, workspace,
+                                           workspace_bytes, hip_stream)
+
+
+def lf_distil(rows, classes, top, logits, top_logits, top_classes, top_classes_ld, temperature, weight, loss, dlogits,
+              hip_stream=0) -> int:
+    return _lib().lf_distil(rows, classes, top, logits, top_logits, top_classes, top_classes_ld, temperature, weight, loss,
+                            dlogits, hip_stream)
 
 
 def lf_operator_error() -> str:
@@ -165,6 +224,70 @@ class E4M3Matrix:
         return out
 
 
+class E4M3Blocks:
+    """rows x cols values in 8 bits with blocks of 128: `codes` (uint8, [rows][cols rounded up to whole 128], e4m3) and `scales`
+    (uint8, one power of two for 128 columns of a row, or with `tiles` for 128 x 128 values; rows of whole fours).  Bytes as
+    E4M3Matrix's."""
+
+    def __init__(self, rows: int, cols: int, tiles: bool = False, device: str = "cuda:0"):
+        t = _torch()
+        groups = -(-cols // BLOCK)
+        self._set(t.empty((rows, groups * BLOCK), dtype=t.uint8, device=device),
+                  t.empty((-(-rows // BLOCK) if tiles else rows, -(-groups // 4) * 4), dtype=t.uint8, device=device), cols, tiles)
+
+    @classmethod
+    def of(cls, codes, scales, cols: int, tiles: bool = False) -> "E4M3Blocks":
+        """The matrix that codes and scales (uint8 tensors of the shapes above, on one GPU) stand for.  They are
+        not copied."""
+        t = _torch()
+        m = cls.__new__(cls)
+        groups = -(-cols // BLOCK)
+        for name, x, width in (("codes", codes, groups * BLOCK), ("scales", scales, -(-groups // 4) * 4)):
+            if x.dtype != t.uint8 or x.dim() != 2 or x.shape[1] != width or (width > 1 and x.stride(1) != 1):
+                raise LfError(LF_EINVAL, f"{name} of a matrix in blocks of 128 with {cols} columns: uint8 [rows][{width}] with "
+                                         f"contiguous rows is needed, got {x.dtype} {list(x.shape)}")
+        if scales.shape[0] != (-(-codes.shape[0] // BLOCK) if tiles else codes.shape[0]) or codes.device != scales.device:
+            raise LfError(LF_EINVAL, "codes and scales have different rows or devices")
+        m._set(codes, scales, cols, tiles)
+        return m
+
+    def _set(self, codes, scales, cols, tiles):
+        self.codes, self.scales, self.cols, self.tiles = codes, scales, cols, tiles
+        self.rows, self.device = codes.shape[0], codes.device
+        self.shape, self._gpu = (self.rows, cols), codes.get_device()
+        # (the stride of one row or of none says nothing)
+        self._m = lf_matrix(codes.data_ptr(), codes.stride(0) if codes.shape[0] > 1 else max(codes.stride(0), codes.shape[1]),
+                            scales.data_ptr(), scales.stride(0) if scales.shape[0] > 1 else max(scales.stride(0), scales.shape[1]),
+                            LF_MATRIX_E4M3_TILES if tiles else LF_MATRIX_E4M3_128)
+
+    def first(self, rows: int) -> "E4M3Blocks":
+        """The first rows (no copy)."""
+        if rows == self.rows:
+            return self
+        return E4M3Blocks.of(self.codes[:rows], self.scales[:-(-rows // BLOCK) if self.tiles else rows], self.cols, self.tiles)
+
+    def first_columns(self, cols: int) -> "E4M3Blocks":
+        """The first columns (no copy; the rest of the last group that they share belongs to them)."""
+        if cols == self.cols:
+            return self
+        groups = -(-cols // BLOCK)
+        return E4M3Blocks.of(self.codes[:, :groups * BLOCK], self.scales[:, :-(-groups // 4) * 4], cols, self.tiles)
+
+    def save(self, x, transposed: Optional["E4M3Blocks"] = None) -> "E4M3Blocks":
+        """Keep x ([rows][cols], f32 or bf16), and in the same pass x^T in `transposed` ([cols][rows], with tiles if this has them)."""
+        _enqueue(self._gpu, _lib().lf_block_save, self.rows, self.cols, _matrix("x", x, self.shape, self._gpu, lf_matrix()), self._m,
+                 _matrix("transposed", transposed, (self.cols, self.rows), self._gpu, lf_matrix()))
+        return self
+
+    def load(self, out=None, dtype="bf16"):
+        """The values, in `out` or a new tensor of the type."""
+        if out is None:
+            out = _torch().empty(self.shape, dtype=_storage(dtype)[0], device=self.device)
+        _enqueue(self._gpu, _lib().lf_block_load, self.rows, self.cols, self._m,
+                 _matrix("out", out, self.shape, self._gpu, lf_matrix()))
+        return out
+
+
 _raw_stream = _current_gpu = None
 
 
@@ -196,7 +319,7 @@ def _matrix(name, x, shape, gpu, m):
     global _TYPES
     if x is None:
         return None
-    if type(x) is E4M3Matrix:
+    if type(x) is E4M3Matrix or type(x) is E4M3Blocks:
         if x.shape != shape or x._gpu != gpu:
             raise LfError(LF_EINVAL, f"{name}: {shape[0]} x {shape[1]} on GPU {gpu} is needed, got {x.shape} on {x.device}")
         return x._m
@@ -255,12 +378,15 @@ class _Operator:
         self._whole = {}                                   # lf_matrix of an output of all rows
 
     def _new(self, name, rows, cols, kind):
-        """An output: a matrix of the storage type or, "e4m3", in 8 bits; None for "none"; a matrix of the caller's is taken as it is."""
+        """An output: a matrix of the storage type or in 8 bits ("e4m3", and "e4m3_128" in blocks of 128); None for "none"; a matrix of
+        the caller's is taken as it is."""
         if isinstance(kind, str) and kind == "none":
             return None
         if isinstance(kind, str) and kind == "e4m3":
             kind = E4M3Matrix(rows, cols, self.device)
-        elif not isinstance(kind, (_torch().Tensor, E4M3Matrix)):
+        elif isinstance(kind, str) and kind == "e4m3_128":
+            kind = E4M3Blocks(rows, cols, device=self.device)
+        elif not isinstance(kind, (_torch().Tensor, E4M3Matrix, E4M3Blocks)):
             kind = _torch().empty((rows, cols), dtype=_storage(kind)[0], device=self.device)
         self._whole[name] = _matrix(name, kind, (rows, cols), self._gpu, lf_matrix())
         return kind
@@ -269,7 +395,7 @@ class _Operator:
         """(the first n rows of an output, their lf_matrix)"""
         if n == self.rows or whole is None:
             return whole, self._whole.get(name)
-        part = whole.first(n) if isinstance(whole, E4M3Matrix) else whole[:n]
+        part = whole.first(n) if isinstance(whole, (E4M3Matrix, E4M3Blocks)) else whole[:n]
         return part, _matrix(name, part, (n, whole.shape[1]), self._gpu, lf_matrix())
 
     def _scratch(self, nbytes):
@@ -338,6 +464,74 @@ class RmsNorm(_Operator):
         _enqueue(gpu, _lib().lf_norm_backward, n, c, _matrix("dy", dy, shape, gpu, m[0]), _matrix("stored", stored, shape, gpu, m[1]),
                  self._kept_gain.address(self._gain), _vector("rstd", rstd, n, gpu), _matrix("dsum", dsum, shape, gpu, m[2]), mdx,
                  self.dgain.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes)
+        return self.dx
+
+
+class LayerNorm(_Operator):
+    """Layer norm with the residual's addition:  sum = x + branch,  y = (sum - mean) / deviation * gain + shift.
+
+    gain, shift: f32 [cols], ones and zeros at first.  out: type of y, dtype, "e4m3" or "e4m3_128".  After `forward`: sum, y (a tensor,
+    an E4M3Matrix or an E4M3Blocks), mean, rstd.  After `backward`: dx (the gradient of x and of branch), dgain, dshift.  out, sum and
+    dx may be matrices of the caller's, as RmsNorm's."""
+
+    def __init__(self, rows: int, cols: int, dtype="bf16", out=None, eps: float = 1e-5, passes: str = "both", sum=None,
+                 dx=None, device: str = "cuda:0"):
+        super().__init__(rows, dtype, passes, device)
+        t = _torch()
+        self.cols, self.eps = cols, eps
+        f32 = dict(dtype=t.float32, device=self.device)
+        self.gain, self.shift = t.ones(cols, **f32), t.zeros(cols, **f32)
+        self._sum = self._y = self._dx = self.sum = self.y = self.dx = self.mean = self.rstd = self.dgain = self.dshift = None
+        if self._forward:
+            self._sum = self._new("sum", rows, cols, self.dtype if sum is None else sum)
+            self._y = self._new("out", rows, cols, self.dtype if out is None else out)
+            self._mean, self._rstd = t.empty(rows, **f32), t.empty(rows, **f32)
+        if self._backward:
+            self._dx = self._new("dx", rows, cols, self.dtype if dx is None else dx)
+            self.dgain, self.dshift = t.empty(cols, **f32), t.empty(cols, **f32)
+            self.workspace_bytes = lf_layer_norm_workspace_bytes(rows, cols)
+            self._workspace = self._scratch(self.workspace_bytes)
+
+    @property
+    def gain(self):
+        return self._gain
+
+    @gain.setter
+    def gain(self, gain):
+        self._gain, self._kept_gain = gain, _Kept("gain", gain, self.cols, self._gpu)
+
+    @property
+    def shift(self):
+        return self._shift
+
+    @shift.setter
+    def shift(self, shift):
+        self._shift, self._kept_shift = shift, _Kept("shift", shift, self.cols, self._gpu)
+
+    def forward(self, x, branch=None):
+        n, c, gpu, m = self._begin(x, self._forward, "forward"), self.cols, self._gpu, self._in
+        self.sum, msum = self._some("sum", self._sum, n)
+        self.y, my = self._some("out", self._y, n)
+        whole = n == self.rows
+        self.mean, self.rstd = self._mean if whole else self._mean[:n], self._rstd if whole else self._rstd[:n]
+        shape = (n, c)
+        _enqueue(gpu, _lib().lf_layer_norm_forward, n, c, _matrix("x", x, shape, gpu, m[0]), _matrix("branch", branch, shape, gpu, m[1]),
+                 self._kept_gain.address(self._gain), self._kept_shift.address(self._shift), self.eps, msum, my,
+                 self._mean.data_ptr(), self._rstd.data_ptr())
+        return self.y
+
+    def backward(self, dy, dsum=None, stored=None, mean=None, rstd=None):
+        """From dy and the gradient that reaches the sum on other ways.  stored: the sum, if not the last forward pass's,
+        in the storage type or in an E4M3Matrix; mean and rstd likewise."""
+        n, c, gpu, m = self._begin(dy, self._backward, "backward"), self.cols, self._gpu, self._in
+        stored = self.sum if stored is None else stored
+        mean, rstd = self.mean if mean is None else mean, self.rstd if rstd is None else rstd
+        self.dx, mdx = self._some("dx", self._dx, n)
+        shape = (n, c)
+        _enqueue(gpu, _lib().lf_layer_norm_backward, n, c, _matrix("dy", dy, shape, gpu, m[0]), _matrix("stored", stored, shape, gpu, m[1]),
+                 self._kept_gain.address(self._gain), _vector("mean", mean, n, gpu), _vector("rstd", rstd, n, gpu),
+                 _matrix("dsum", dsum, shape, gpu, m[2]), mdx, self.dgain.data_ptr(), self.dshift.data_ptr(),
+                 self._workspace.data_ptr(), self.workspace_bytes)
         return self.dx
 
 
@@ -413,3 +607,135 @@ class Linear(_Operator):
                  _matrix("z", z, (n, o), gpu, m[1]), self._act, _matrix("x", x, (n, i), gpu, m[2]),
                  self._weights(), mdx, self._whole["dw"], self.db.data_ptr(), self._workspace.data_ptr(), self.workspace_bytes)
         return self.dx
+
+
+class BlockLinear(_Operator):
+    """Matrix product with bias, activation and residual of operands in 8 bits with blocks of 128:  z = x w^T + b,  y = act(z) + residual.
+
+    `set_params` keeps the weights in 8 bits (w8, and w8_t for the backward pass), `refresh` does so again after they have changed.
+    x is put into 8 bits in the pass; with passes="both" its transposed codes are kept for the backward pass (x_t), an eighth
+    to a quarter of what x took.  x that is an E4M3Blocks already is taken as it is, and x_t is the caller's then.  y: storage type or
+    "e4m3_128"; z, what the backward pass needs of an activation: the same, or "none"; dw: dtype or "f32".  After `forward`: y, z, x_t.
+    After `backward`: dx, dw, db.  y, z, dx, dw and workspace may be the caller's, as Linear's."""
+
+    def __init__(self, rows: int, outputs: int, inputs: int, dtype="bf16", act: str = "none", y=None, z="none", dx=None,
+                 dw=None, workspace=None, passes: str = "both", device: str = "cuda:0"):
+        super().__init__(rows, dtype, passes, device)
+        if act not in ACTIVATIONS:
+            raise LfError(LF_EINVAL, f"activation {act!r}: one of {sorted(ACTIVATIONS)}")
+        t = _torch()
+        self.outputs, self.inputs, self._act = outputs, inputs, ACTIVATIONS[act]
+        self.w = self.b = self.w8 = self.w8_t = self.y = self.z = self.dx = self.dw = self.db = self.x_t = self._x_t = None
+        nbytes = 0
+        if self._forward:
+            self._y = self._new("y", rows, outputs, self.dtype if y is None else y)
+            self._z = self._new("z", rows, outputs, z)
+            nbytes = lf_block_linear_workspace_bytes(rows, outputs, inputs)
+            if self._backward:
+                self._x_t = E4M3Blocks(inputs, rows, device=self.device)
+        if self._backward:
+            self._dx = self._new("dx", rows, inputs, self.dtype if dx is None else dx)
+            self.dw = self._new("dw", outputs, inputs, self.dtype if dw is None else dw)
+            self.db = t.empty(outputs, dtype=t.float32, device=self.device)
+            nbytes = max(nbytes, lf_block_linear_backward_workspace_bytes(rows, outputs, inputs))
+        self.workspace_bytes = nbytes
+        if workspace is not None and (workspace.dtype != t.uint8 or workspace.get_device() != self._gpu
+                                      or not workspace.is_contiguous() or workspace.numel() < nbytes):
+            raise LfError(LF_EINVAL, f"workspace: {nbytes} contiguous uint8 on GPU {self._gpu} are needed")
+        self._workspace = self._scratch(nbytes) if workspace is None else workspace
+
+    def set_params(self, w, b=None, w_t=None) -> None:
+        """Register w ([outputs][inputs], f32 or bf16) and b ([outputs] f32, or None), and keep w in 8 bits.  w and b are kept by reference:
+        after w has changed, `refresh`.  w may be in 8 bits already, an E4M3Blocks with tiles; the backward pass needs w_t then, its
+        transposed."""
+        kept = _Kept("b", b, self.outputs, self._gpu)
+        shape, gpu = (self.outputs, self.inputs), self._gpu
+        if isinstance(w, E4M3Blocks):
+            _matrix("w", w, shape, gpu, lf_matrix())
+            if self._backward and not isinstance(w_t, E4M3Blocks):
+                raise LfError(LF_EINVAL, "w_t: the backward pass takes weights in 8 bits transposed")
+            _matrix("w_t", w_t, shape[::-1], gpu, lf_matrix())
+            self.w, self.w8, self.w8_t = None, w, w_t if self._backward else None
+        else:
+            _matrix("w", w, shape, gpu, lf_matrix())
+            if w_t is not None:
+                raise LfError(LF_EINVAL, "w_t goes with weights in 8 bits")
+            # (matrices of the caller's, of an earlier call, are left as they are)
+            if self.w is None:
+                self.w8 = E4M3Blocks(*shape, tiles=True, device=self.device) if self._forward else None
+                self.w8_t = E4M3Blocks(*shape[::-1], tiles=True, device=self.device) if self._backward else None
+            self.w = w
+        self.b, self._kept_b = b, kept
+        self.refresh()
+
+    def refresh(self) -> None:
+        """Keep the weights as they are now in 8 bits.  (Weights that were given in 8 bits are read as they lie.)"""
+        if self.w is None:
+            if self.w8 is None and self.w8_t is None:
+                raise LfError(LF_EINVAL, "w is NULL: set_params gives the weights")
+            return
+        _enqueue(self._gpu, _lib().lf_block_save, self.outputs, self.inputs,
+                 _matrix("w", self.w, (self.outputs, self.inputs), self._gpu, lf_matrix()), self.w8 and self.w8._m, self.w8_t and self.w8_t._m)
+
+    def _weights(self, w8):
+        if w8 is None:
+            raise LfError(LF_EINVAL, "w is NULL: set_params gives the weights")
+        return w8._m
+
+    def forward(self, x, residual=None):
+        n, o, i, gpu, m = self._begin(x, self._forward, "forward"), self.outputs, self.inputs, self._gpu, self._in
+        self.y, my = self._some("y", self._y, n)
+        self.z, mz = self._some("z", self._z, n)
+        self.x_t = None if self._x_t is None or isinstance(x, E4M3Blocks) else self._x_t.first_columns(n)
+        _enqueue(gpu, _lib().lf_block_linear_forward, n, o, i, _matrix("x", x, (n, i), gpu, m[0]), self._weights(self.w8),
+                 self._kept_b.address(self.b), self._act, _matrix("residual", residual, (n, o), gpu, m[1]), my, mz,
+                 None if self.x_t is None else self.x_t._m, self._workspace.data_ptr(), self.workspace_bytes)
+        return self.y
+
+    def backward(self, dy, x_t=None, z=None):
+        """From dy, the transposed input of the forward pass (E4M3Blocks, [inputs][rows]) and z, if they are not the last forward pass's.
+        Without an activation z is not looked at."""
+        n, o, i, gpu, m = self._begin(dy, self._backward, "backward"), self.outputs, self.inputs, self._gpu, self._in
+        x_t = self.x_t if x_t is None else x_t
+        z = None if self._act == LF_ACT_NONE else self.z if z is None else z
+        self.dx, mdx = self._some("dx", self._dx, n)
+        _enqueue(gpu, _lib().lf_block_linear_backward, n, o, i, _matrix("dy", dy, (n, o), gpu, m[0]), _matrix("z", z, (n, o), gpu, m[1]),
+                 self._act, _matrix("x_t", x_t, (i, n), gpu, m[2]), self._weights(self.w8_t), mdx, self._whole["dw"], self.db.data_ptr(),
+                 self._workspace.data_ptr(), self.workspace_bytes)
+        return self.dx
+
+
+class Distillation(_Operator):
+    """Distillation loss of each row from a teacher's top logits:  p = softmax(t / T) over the row's `top` entries,
+    q = softmax(logits / T) over the classes,  loss = weight T^2 sum p (log p - log q),  and its gradient in the same pass.
+
+    passes: "both", or "forward" for the loss alone.  After `forward`: loss (f32), dlogits (the gradient of the rows' losses, their
+    weights in it).  dlogits may be a matrix of the caller's to write to, the logits of the call themselves among them."""
+
+    def __init__(self, rows: int, classes: int, top: int, dtype="bf16", temperature: float = 1.0, passes: str = "both", dlogits=None,
+                 device: str = "cuda:0"):
+        super().__init__(rows, dtype, passes, device)
+        if not self._forward:
+            raise LfError(LF_EINVAL, f"passes = {passes!r}: forward or both (the gradient is the loss's pass's)")
+        self.classes, self.top, self.temperature = classes, top, temperature
+        self.loss = self.dlogits = self._dlogits = None
+        self._loss = _torch().empty(rows, dtype=_torch().float32, device=self.device)
+        if self._backward:
+            self._dlogits = self._new("dlogits", rows, classes, self.dtype if dlogits is None else dlogits)
+
+    def forward(self, logits, top_logits, top_classes, weight=None):
+        """top_logits: [rows][top], f32 or bf16; top_classes: [rows][top] int32, negative where there is no entry; weight: [rows] f32, None
+        for ones."""
+        n, gpu, m = self._begin(logits, True, "forward"), self._gpu, self._in
+        shape = (n, self.top)
+        if (top_classes.dtype != _torch().int32 or top_classes.shape != shape or top_classes.get_device() != gpu
+                or (self.top > 1 and top_classes.stride(1) != 1)):
+            raise LfError(LF_EINVAL, f"top_classes: {n} x {self.top} int32 with contiguous rows on GPU {gpu} are needed, got "
+                                     f"{list(top_classes.shape)}, {top_classes.dtype}, on {top_classes.device}")
+        self.loss = self._loss if n == self.rows else self._loss[:n]
+        self.dlogits, mdl = self._some("dlogits", self._dlogits, n)
+        _enqueue(gpu, _lib().lf_distil, n, self.classes, self.top, _matrix("logits", logits, (n, self.classes), gpu, m[0]),
+                 _matrix("top_logits", top_logits, shape, gpu, m[1]), top_classes.data_ptr(),
+                 top_classes.stride(0) if n > 1 else max(top_classes.stride(0), self.top), self.temperature,
+                 _vector("weight", weight, n, gpu), self._loss.data_ptr(), mdl)
+        return self.loss
