@@ -12,6 +12,7 @@
 #include "column_sums.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lf {
 namespace ops {
@@ -117,21 +118,44 @@ __device__ __forceinline__ void values_of(const v8i& codes, int byte, v8bf (&v)[
         }
 }
 
+__device__ __forceinline__ void load_dwords_to_lds(v4i resource, unsigned voffset, unsigned soffset, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+                 :
+                 : "s"(lds), "v"(voffset), "s"(resource), "s"(soffset)
+                 : "memory");
+}
+
 template <int BM, int BN, int WM, int WN>
 struct Shape {
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, MT = BM / WM / 32, NT = BN / WN / 32;
     static constexpr int kStage = (BM + BN) * kBlock;                  // bytes of a k-tile of both operands
     static constexpr int kPieces = (BM + BN) / 8 / kWaves;             // loads of a wave for it, 8 rows each
     static constexpr int kPiecesM = BM / 8 / kWaves;
+    static constexpr int kScales = (BM + BN) * 4;                      // bytes of four k-tiles' scales, a row's next to each other
+    static constexpr int kScalesAt = 2 * kStage;
     static constexpr int kFlatRows = WM * 16, kFlatLd = BN + 4;        // the epilogue's staging
-    static constexpr int kBytes = std::max(2 * kStage, 2 * kFlatRows * kFlatLd * 4);
+    static constexpr int kBytes = std::max(2 * (kStage + kScales), 2 * kFlatRows * kFlatLd * 4);
     static_assert(kPiecesM * 8 * kWaves == BM && kPieces * 8 * kWaves == BM + BN, "whole pieces for every wave");
     static_assert((kWaves * 4) % 8 == 0, "the places of a lane's pieces are the same in all of its loads");
 };
 
+// f(0), f(1), ... f(N - 1), each with its number known when it is compiled, and nothing moved from one to another.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void in_order(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        __builtin_amdgcn_sched_barrier(0);
+        in_order<N, I + 1>(f);
+    }
+}
+
 // A tile in LDS: rows of 128 bytes, eight pieces of 16, piece p of row i at place p ^ (i / 2 % 8), so that the pieces of 16 rows, which LDS
 // serves at once, lie in different banks.  The load to LDS puts lane after lane, so a lane asks for the piece that belongs to its
 // place.  Rows past the operand's last are the last again, which nothing looks at.
+//
+// What bounds it is LDS next to the matrix cores: a k-tile of 256 x 256 is written once (64 KB) and read by four waves, 128 x 128 each
+// (32 KB a wave): 192 KB, 1536 cycles, while the matrix cores take 2048.  (Eight waves of 64 x 128 would read 192 KB.)  One wave a matrix core
+// then: what it issues next to the multiplications is placed between them, instruction by instruction.
 template <int BM, int BN, int WM, int WN, bool EXACT>
 __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint8_t* lds) {
     typedef Shape<BM, BN, WM, WN> S;
@@ -163,21 +187,22 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
         const v4i res_q = resource_of((const uint8_t*)g.Q.p + (long long)n0 * g.Q.ld, last_q * ld_q + row_bytes);
         const unsigned base = lds_address(lds), row_in = wave * 8 + lane / 8;
         const unsigned piece = ((lane & 7) ^ ((row_in >> 1) & 7)) * 16;
-        const unsigned first_p = row_in * ld_p, first_q = row_in * ld_q;
-        auto request = [&](int turn, unsigned buffer) {
+        unsigned first_p = row_in * ld_p, first_q = row_in * ld_q;
+        // load u of a wave's for a k-tile (what is below is not worth a register each from k-tile to k-tile)
+        auto request = [&](int turn, unsigned buffer, auto which) {
+            constexpr int u = which(), of = u < S::kPiecesM ? u : u - S::kPiecesM;
+            constexpr bool p = u < S::kPiecesM;
             const unsigned k = (unsigned)(kt0 + turn) * kBlock;
-#pragma unroll
-            for (int u = 0; u < S::kPieces; ++u) {
-                const bool p = u < S::kPiecesM;
-                const unsigned v = p ? min(first_p + u * kWaves * 8 * ld_p, last_p * ld_p) : min(first_q + (u - S::kPiecesM) * kWaves * 8 * ld_q, last_q * ld_q);
-                load_to_lds(p ? res_p : res_q, v + piece, k, base + buffer + (u * kWaves + wave) * 1024);
-            }
+            const unsigned v = p ? min(first_p + of * kWaves * 8 * ld_p, last_p * ld_p) : min(first_q + of * kWaves * 8 * ld_q, last_q * ld_q);
+            load_to_lds(p ? res_p : res_q, v + piece, k, base + buffer + (u * kWaves + wave) * 1024);
         };
         // codes past the contraction's end become zeros (in the last k-tile)
         const int tail = g.K - (g.k_tiles - 1) * kBlock;
         auto mend = [&](int turn, unsigned buffer) {
             if (tail == kBlock || kt0 + turn != g.k_tiles - 1) return;
-            for (int i = t; i < (BM + BN) * 8; i += kThreads) {
+            int first = t;
+            asm volatile("" : "+v"(first));
+            for (int i = first; i < (BM + BN) * 8; i += kThreads) {
                 const int row = i / 8, p = i % 8;
                 v4u* at = reinterpret_cast<v4u*>(lds + buffer + row * kBlock + ((p ^ (row >> 1)) & 7) * 16);
                 if (p * 16 + 16 > tail) {
@@ -188,92 +213,142 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
             }
             wait_and_meet();
         };
-        // scales: four k-tiles' in a register, the next four's under way
-        const uint8_t* scales_p[MT];
-        const uint8_t* scales_q[NT];
+        // Scales: four k-tiles' of every row in LDS, loaded with the first of the four.  A row's of a matrix of tiles is its block's.
+        const int scale_p0 = m0 >> g.p_shift, scale_q0 = n0 >> g.q_shift, four_bytes = (ceil_div(g.K, kBlock) + 3) / 4 * 4;
+        const int scale_ld_p = (int)g.P.scale_ld, scale_ld_q = (int)g.Q.scale_ld;
+        const v4i res_sp = resource_of(g.P.scales + (long long)scale_p0 * scale_ld_p, (((m0 + last_p) >> g.p_shift) - scale_p0) * scale_ld_p + four_bytes);
+        const v4i res_sq = resource_of(g.Q.scales + (long long)scale_q0 * scale_ld_q, (((n0 + last_q) >> g.q_shift) - scale_q0) * scale_ld_q + four_bytes);
+        auto request_scales = [&](int turn) {
+            const unsigned four = (unsigned)(kt0 + turn) >> 2, to = base + S::kScalesAt + (four & 1) * S::kScales;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) scales_p[i] = g.P.scales + (long long)(min(m0 + wm + 32 * i + r32, g.M - 1) >> g.p_shift) * g.P.scale_ld;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) scales_q[j] = g.Q.scales + (long long)(min(n0 + wn + 32 * j + r32, g.N - 1) >> g.q_shift) * g.Q.scale_ld;
-        int four_p[MT], four_q[NT];
-        auto scales = [&](int turn) {
-            const int at = (kt0 + turn) & ~3;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) four_p[i] = *as_global<const int>(scales_p[i] + at);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) four_q[j] = *as_global<const int>(scales_q[j] + at);
-        };
-        // an operand of one step, 64 q: lane holds 32 q of row r32, pieces 4 step + 2 half and the next
-        const unsigned turn_p = ((r32 >> 1) & 7), at_p = (wm + r32) * kBlock, at_q = (BM + wn + r32) * kBlock;
-        v8i a[2][MT], q[2][NT];
-        auto read = [&](int step, unsigned buffer, v8i (&fa)[MT], v8i (&fq)[NT]) {
-            const unsigned lo = ((4 * step + 2 * half) ^ turn_p) * 16, hi = lo ^ 16;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const v4i x = *reinterpret_cast<const v4i*>(lds + buffer + at_p + lo + 32 * i * kBlock);
-                const v4i y = *reinterpret_cast<const v4i*>(lds + buffer + at_p + hi + 32 * i * kBlock);
-                fa[i] = v8i{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            for (int d = wave; d < (BM + BN) / 64; d += kWaves) {
+                unsigned row = d * 64 + lane;
+                asm volatile("" : "+v"(row));
+                const bool p = d * 64 < BM;
+                const unsigned v = p ? (((m0 + min(row, last_p)) >> g.p_shift) - scale_p0) * scale_ld_p
+                                     : (((n0 + min(row - BM, last_q)) >> g.q_shift) - scale_q0) * scale_ld_q;
+                load_dwords_to_lds(p ? res_sp : res_sq, v, four * 4, to + d * 256);
             }
+        };
+        int sp[MT], sq[NT], next_sp[MT], next_sq[NT];
+        auto read_scale = [&](int turn, auto which) {
+            constexpr int i = which();
+            const unsigned k = (unsigned)(kt0 + turn);
+            const uint8_t* at = lds + S::kScalesAt + (k >> 2 & 1) * S::kScales + (k & 3) + r32 * 4;
+            if constexpr (i < MT) next_sp[i] = at[(wm + 32 * i) * 4];
+            else next_sq[i - MT] = at[(BM + wn + 32 * (i - MT)) * 4];
+        };
+        auto take_scales = [&]() {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sp[i] = next_sp[i];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sq[j] = next_sq[j];
+        };
+        // An operand of one step, 64 q: lane holds 32 q of row r32, pieces 4 step + 2 half and the next.  Read r of a step's.
+        const unsigned turn_p = (r32 >> 1) & 7, at_p = (wm + r32) * kBlock, at_q = (BM + wn + r32) * kBlock;
+        v8i a[2][MT], q[2][NT];
+        auto read = [&](auto step, unsigned buffer, auto which) {
+            constexpr int r = which(), i = r / 2, high = r % 2;
+            const unsigned place = (((4 * step() + 2 * half) ^ turn_p) ^ high) * 16;
+            const v4i x = *reinterpret_cast<const v4i*>(lds + buffer + (i < MT ? at_p : at_q) + place + 32 * (i < MT ? i : i - MT) * kBlock);
+            v8i& to = i < MT ? a[step()][i < MT ? i : 0] : q[step()][i < MT ? 0 : i - MT];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[4 * high + e] = x[e];
+        };
+        auto multiply = [&](auto step, auto which) {
+            constexpr int i = which() / NT, j = which() % NT;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[step()][i], q[step()][j], acc[i][j], 0, 0, 0, sp[i], 0, sq[j]);
+        };
+        auto multiply_exactly = [&](auto step) {
+            v8bf x[MT][4];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) values_of(a[step()][i], sp[i], x[i]);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const v4i x = *reinterpret_cast<const v4i*>(lds + buffer + at_q + lo + 32 * j * kBlock);
-                const v4i y = *reinterpret_cast<const v4i*>(lds + buffer + at_q + hi + 32 * j * kBlock);
-                fq[j] = v8i{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                v8bf y[4];
+                values_of(q[step()][j], sq[j], y);
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][h], y[h], acc[i][j], 0, 0, 0);
             }
         };
-        int sp[MT], sq[NT];
-        auto multiply = [&](const v8i (&fa)[MT], const v8i (&fq)[NT]) {
-            if constexpr (EXACT) {
-                v8bf x[MT][4];
-#pragma unroll
-                for (int i = 0; i < MT; ++i) values_of(fa[i], sp[i], x[i]);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    v8bf y[4];
-                    values_of(fq[j], sq[j], y);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][h], y[h], acc[i][j], 0, 0, 0);
-                }
-                return;
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fq[j], acc[i][j], 0, 0, 0, sp[i], 0, sq[j]);
+        constexpr std::integral_constant<int, 0> s0;
+        constexpr std::integral_constant<int, 1> s1;
+        constexpr int kMfmas = MT * NT, kReads = 2 * (MT + NT), kScaleReads = MT + NT, kLoads = S::kPieces;
+        // which of N instructions follow multiplication f, if all of them are to be out after WINDOW multiplications
+        const auto share = [](auto n, auto window, auto f, auto&& one) {
+            constexpr int N = n(), W = window(), F = f(), from = F < W ? N * F / W : N, to = F < W ? N * (F + 1) / W : N;
+            one(std::integral_constant<int, from>(), std::integral_constant<int, to - from>());
         };
-        auto shift = [&](int turn) {
-            const int by = ((kt0 + turn) & 3) * 8;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) sp[i] = four_p[i] >> by;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sq[j] = four_q[j] >> by;
+        const auto some = [](auto from, auto count, auto&& f) {
+            constexpr int FROM = from(), COUNT = count();
+            if constexpr (COUNT > 0) f(std::integral_constant<int, FROM>());
+            if constexpr (COUNT > 1) f(std::integral_constant<int, FROM + 1>());
+            if constexpr (COUNT > 2) f(std::integral_constant<int, FROM + 2>());
+            if constexpr (COUNT > 3) f(std::integral_constant<int, FROM + 3>());
+            if constexpr (COUNT > 4) f(std::integral_constant<int, FROM + 4>());
+            static_assert(COUNT <= 5);
         };
+        constexpr std::integral_constant<int, kReads> reads;
+        constexpr std::integral_constant<int, kScaleReads> scale_reads;
+        constexpr std::integral_constant<int, kLoads> loads;
+        constexpr std::integral_constant<int, (kMfmas + 1) / 2> early;
+        constexpr std::integral_constant<int, kMfmas - (kMfmas > 4 ? kMfmas / 4 : 1)> most;
         // A k-tile is in LDS, the next on its way to the other half of it.  The barrier stands between a k-tile's two steps: by then
         // every wave has the second step's operands in registers, the half is free for the k-tile after the next, and the next
         // k-tile's first operands are read while the second step is multiplied.
-        scales(0);
-        request(0, 0);
+        request_scales(0);
+        if (((kt0 + 1) & 3) == 0) request_scales(1);
+        in_order<kLoads>([&](auto u) { request(0, 0, u); });
         wait_and_meet();
         mend(0, 0);
-        if (turns > 1) request(1, S::kStage);
-        read(0, 0, a[0], q[0]);
+        in_order<kLoads>([&](auto u) { request(min(1, turns - 1), S::kStage, u); });
+        in_order<kScaleReads>([&](auto i) { read_scale(0, i); });
+        in_order<kReads>([&](auto r) { read(s0, 0, r); });
         unsigned buffer = 0;
         for (int turn = 0; turn < turns; ++turn) {
-            shift(turn);
-            read(1, buffer, a[1], q[1]);
-            multiply(a[0], q[0]);
+            asm volatile("" : "+v"(first_p), "+v"(first_q));
+            take_scales();
+            if constexpr (EXACT) {
+                in_order<kReads>([&](auto r) { read(s1, buffer, r); });
+                multiply_exactly(s0);
+            } else {
+                in_order<kMfmas>([&](auto f) {
+                    multiply(s0, f);
+                    share(reads, most, f, [&](auto from, auto count) { some(from, count, [&](auto r) { read(s1, buffer, r); }); });
+                });
+            }
+            // (the first step's multiplications stay on this side of the barrier)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    if constexpr (BM == 256) asm volatile("" : "+a"(acc[i][j]));
+                    else asm volatile("" : "+v"(acc[i][j]));
+                }
             wait_and_meet();
             mend(turn + 1, buffer ^ S::kStage);
-            if (((kt0 + turn + 1) & 3) == 0) scales(turn + 1);
-            if (turn + 2 < turns) request(turn + 2, buffer);
-            read(0, buffer ^ S::kStage, a[0], q[0]);
-            multiply(a[1], q[1]);
+            // (past the last k-tile the last is loaded again, and what lies in LDS read, which nothing looks at: a branch around a part of this
+            // would cost the sums a second set of registers)
+            const int after = min(turn + 2, turns - 1);
+            if (((kt0 + turn + 2) & 3) == 0) request_scales(after);
+            if constexpr (EXACT) {
+                in_order<kLoads>([&](auto u) { request(after, buffer, u); });
+                in_order<kScaleReads>([&](auto i) { read_scale(turn + 1, i); });
+                in_order<kReads>([&](auto r) { read(s0, buffer ^ S::kStage, r); });
+                multiply_exactly(s1);
+            } else {
+                in_order<kMfmas>([&](auto f) {
+                    multiply(s1, f);
+                    share(loads, early, f, [&](auto from, auto count) { some(from, count, [&](auto u) { request(after, buffer, u); }); });
+                    share(scale_reads, early, f, [&](auto from, auto count) { some(from, count, [&](auto i) { read_scale(turn + 1, i); }); });
+                    share(reads, most, f, [&](auto from, auto count) { some(from, count, [&](auto r) { read(s0, buffer ^ S::kStage, r); }); });
+                });
+            }
             buffer ^= S::kStage;
         }
-        __syncthreads();          // LDS becomes the epilogue's
+        wait_and_meet();          // LDS becomes the epilogue's
     }
 
     // Accumulator element e of lane (r32, half) of square (i, j) is C[.. 32 i + 8 (e / 4) + 4 half + e % 4][.. 32 j + r32].  Rows turn through LDS, 16 of
@@ -308,7 +383,7 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
 }
 
 template <int BM, int BN, int WM, int WN, bool EXACT>
-__global__ __launch_bounds__(64 * WM * WN) void k_block_product(const Args g) {
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(BM == 256 ? 1 : 2, BM == 256 ? 1 : 2))) void k_block_product(const Args g) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[Shape<BM, BN, WM, WN>::kBytes];
     product_tile<BM, BN, WM, WN, EXACT>(g, blockIdx.x, lds);
 }
@@ -548,10 +623,10 @@ hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
     const Args a = args_of(g, p);
     const dim3 grid((unsigned)a.tiles_m * a.tiles_n * a.splits);
     if (exact(g.f)) {
-        if (p.tile == 256) k_block_product<256, 256, 4, 2, true><<<grid, 512, 0, s>>>(a);
+        if (p.tile == 256) k_block_product<256, 256, 2, 2, true><<<grid, 256, 0, s>>>(a);
         else k_block_product<128, 128, 2, 2, true><<<grid, 256, 0, s>>>(a);
     } else {
-        if (p.tile == 256) k_block_product<256, 256, 4, 2, false><<<grid, 512, 0, s>>>(a);
+        if (p.tile == 256) k_block_product<256, 256, 2, 2, false><<<grid, 256, 0, s>>>(a);
         else k_block_product<128, 128, 2, 2, false><<<grid, 256, 0, s>>>(a);
     }
     const hipError_t e = hipGetLastError();
