@@ -32,15 +32,13 @@ __device__ __forceinline__ void times_slope(int act, float (&d)[8], const float 
     }
 }
 
-// v / 2^(byte - 127) as a number that the conversion takes: a group whose scale is the largest holds at most 240 of it (256 would
-// be no finite number), infinities and NaN become NaN.
+__device__ __forceinline__ unsigned finite_bits(float v) { return __float_as_uint(finite_magnitude(v)); }
+// v / 2^(byte - 127) as the conversion takes it where a group holds what is not finite, which becomes NaN, or has the largest scale, of
+// which it holds at most 240 (256 would be no finite number).
 __device__ __forceinline__ float scaled(float v, int byte) {
-    const float a = v * scale_power(254 - byte);
-    if (byte < kLargestScale && fabsf(v) < __builtin_inff()) return a;
-    const float most = byte == kLargestScale ? 240.0f : 448.0f;
+    const float a = v * scale_power(254 - byte), most = byte == kLargestScale ? 240.0f : 448.0f;
     return fabsf(v) < __builtin_inff() ? fminf(fmaxf(a, -most), most) : __builtin_nanf("");
 }
-__device__ __forceinline__ unsigned finite_bits(float v) { return __float_as_uint(finite_magnitude(v)); }
 
 // A workgroup keeps a block of 128 x 128 values in registers, thread t eight rows (8 (t / 16) and on) of eight columns (8 (t % 16) and
 // on).  A row's group is 16 lanes' chunks, so its scale is a maximum over a row of lanes; a column's is one over the thread's
@@ -112,8 +110,12 @@ __global__ __launch_bounds__(kThreads) void k_block_save(const BlockSave a, int 
 #pragma unroll
         for (int j = 0; j < 8; ++j) tops[down][across * kChunk + j] = down_top[j];
     }
+    // (every value finite and no group of the largest scale: nothing to look at value by value)
+    unsigned most = 0;
+#pragma unroll
+    for (int i = 0; i < kHigh; ++i) most = max(most, own[i]);
+    const bool rare = __syncthreads_or(odd || scale_byte(__uint_as_float(most)) >= kLargestScale);
     int tile_byte = 0;
-    __syncthreads();
     if constexpr (TILES) {
         unsigned m = 0;
         for (int i = 0; i < kThreads / kAcross; ++i) m = max(m, tops[i][t % kBlock]);
@@ -148,9 +150,14 @@ __global__ __launch_bounds__(kThreads) void k_block_save(const BlockSave a, int 
 #pragma unroll
         for (int i = 0; i < kHigh; ++i) {
             const int byte = TILES ? tile_byte : scale_byte(__uint_as_float(sixteen_max(own[i])));
+            const float inverse = scale_power(254 - byte);
             float s[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] = scaled(v[i][j], byte);
+            for (int j = 0; j < 8; ++j) s[j] = v[i][j] * inverse;
+            if (rare) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] = scaled(v[i][j], byte);
+            }
             if (row + i < a.rows) {
                 *as_global<v2u>((uint8_t*)a.out.p + (long long)(row + i) * a.out.ld + col) = convert_eight(s);
                 if (!TILES && across == 0) *as_global<uint8_t>(a.out.scales + (long long)(row + i) * a.out.scale_ld + bx) = (uint8_t)byte;
@@ -162,9 +169,14 @@ __global__ __launch_bounds__(kThreads) void k_block_save(const BlockSave a, int 
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int c = across * kChunk + j, byte = TILES ? tile_byte : column_byte[c];
+        const float inverse = scale_power(254 - byte);
         float s[8];
 #pragma unroll
-        for (int i = 0; i < kHigh; ++i) s[i] = scaled(v[i][j], byte);
+        for (int i = 0; i < kHigh; ++i) s[i] = v[i][j] * inverse;
+        if (rare) {
+#pragma unroll
+            for (int i = 0; i < kHigh; ++i) s[i] = scaled(v[i][j], byte);
+        }
         *reinterpret_cast<v2u*>(turned + c * kBlock + ((down ^ across) * 8)) = convert_eight(s);
     }
     __syncthreads();

@@ -90,8 +90,10 @@ __device__ __forceinline__ void load_to_lds(v4i resource, unsigned voffset, unsi
                  : "s"(lds), "v"(voffset), "s"(resource), "s"(soffset)
                  : "memory");
 }
+// Until at most LEFT of a wave's loads are on their way, and all waves are here.
+template <int LEFT>
 __device__ __forceinline__ void wait_and_meet() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -128,15 +130,14 @@ __device__ __forceinline__ void load_dwords_to_lds(v4i resource, unsigned voffse
 template <int BM, int BN, int WM, int WN>
 struct Shape {
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, MT = BM / WM / 32, NT = BN / WN / 32;
-    static constexpr int kStage = (BM + BN) * kBlock;                  // bytes of a k-tile of both operands
-    static constexpr int kPieces = (BM + BN) / 8 / kWaves;             // loads of a wave for it, 8 rows each
-    static constexpr int kPiecesM = BM / 8 / kWaves;
-    static constexpr int kScales = (BM + BN) * 4;                      // bytes of four k-tiles' scales, a row's next to each other
-    static constexpr int kScalesAt = 2 * kStage;
+    static constexpr int kPart = (BM + BN) * 64, kParts = 4;           // bytes of 64 q of both operands; so many lie in LDS
+    static constexpr int kPieces = (BM + BN) / 16 / kWaves;            // loads of a wave for them, 16 rows each
+    static constexpr int kPiecesM = BM / 16 / kWaves;
+    static constexpr int kScales = (BM + BN) * 4;                      // bytes of four groups' scales, a row's next to each other
+    static constexpr int kScalesAt = kParts * kPart;
     static constexpr int kFlatRows = WM * 16, kFlatLd = BN + 4;        // the epilogue's staging
-    static constexpr int kBytes = std::max(2 * (kStage + kScales), 2 * kFlatRows * kFlatLd * 4);
-    static_assert(kPiecesM * 8 * kWaves == BM && kPieces * 8 * kWaves == BM + BN, "whole pieces for every wave");
-    static_assert((kWaves * 4) % 8 == 0, "the places of a lane's pieces are the same in all of its loads");
+    static constexpr int kBytes = std::max(kParts * kPart + 2 * kScales, 2 * kFlatRows * kFlatLd * 4);
+    static_assert(kPiecesM * 16 * kWaves == BM && kPieces * 16 * kWaves == BM + BN, "whole pieces for every wave");
 };
 
 // f(0), f(1), ... f(N - 1), each with its number known when it is compiled, and nothing moved from one to another.
@@ -149,11 +150,11 @@ __device__ __forceinline__ void in_order(F&& f) {
     }
 }
 
-// A tile in LDS: rows of 128 bytes, eight pieces of 16, piece p of row i at place p ^ (i / 2 % 8), so that the pieces of 16 rows, which LDS
-// serves at once, lie in different banks.  The load to LDS puts lane after lane, so a lane asks for the piece that belongs to its
-// place.  Rows past the operand's last are the last again, which nothing looks at.
+// 64 q of a tile in LDS, a part: rows of 64 bytes, four pieces of 16, piece p of row i at place p ^ (i / 4 % 4), so that the pieces of 16
+// rows, which LDS serves at once, lie in different banks.  The load to LDS puts lane after lane, so a lane asks for the piece that
+// belongs to its place.  Rows past the operand's last are the last again, which nothing looks at.
 //
-// What bounds it is LDS next to the matrix cores: a k-tile of 256 x 256 is written once (64 KB) and read by four waves, 128 x 128 each
+// What bounds it is LDS next to the matrix cores: 128 q of 256 x 256 are written once (64 KB) and read by four waves, 128 x 128 each
 // (32 KB a wave): 192 KB, 1536 cycles, while the matrix cores take 2048.  (Eight waves of 64 x 128 would read 192 KB.)  One wave a matrix core
 // then: what it issues next to the multiplications is placed between them, instruction by instruction.
 template <int BM, int BN, int WM, int WN, bool EXACT>
@@ -185,35 +186,35 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
         const unsigned row_bytes = (unsigned)whole_blocks(g.K);
         const v4i res_p = resource_of((const uint8_t*)g.P.p + (long long)m0 * g.P.ld, last_p * ld_p + row_bytes);
         const v4i res_q = resource_of((const uint8_t*)g.Q.p + (long long)n0 * g.Q.ld, last_q * ld_q + row_bytes);
-        const unsigned base = lds_address(lds), row_in = wave * 8 + lane / 8;
-        const unsigned piece = ((lane & 7) ^ ((row_in >> 1) & 7)) * 16;
-        unsigned first_p = row_in * ld_p, first_q = row_in * ld_q;
-        // load u of a wave's for a k-tile (what is below is not worth a register each from k-tile to k-tile)
-        auto request = [&](int turn, unsigned buffer, auto which) {
+        const unsigned base = lds_address(lds), row_in = wave * 16 + lane / 4;
+        const unsigned piece = ((lane & 3) ^ ((row_in >> 2) & 3)) * 16;
+        const unsigned first_p = row_in * ld_p, first_q = row_in * ld_q;
+        const int parts = 2 * turns;
+        // load u of a wave's for a part
+        auto request = [&](int part, unsigned slot, auto which) {
             constexpr int u = which(), of = u < S::kPiecesM ? u : u - S::kPiecesM;
             constexpr bool p = u < S::kPiecesM;
-            const unsigned k = (unsigned)(kt0 + turn) * kBlock;
-            const unsigned v = p ? min(first_p + of * kWaves * 8 * ld_p, last_p * ld_p) : min(first_q + of * kWaves * 8 * ld_q, last_q * ld_q);
-            load_to_lds(p ? res_p : res_q, v + piece, k, base + buffer + (u * kWaves + wave) * 1024);
+            const unsigned k = (unsigned)kt0 * kBlock + (unsigned)part * 64;
+            const unsigned v = p ? min(first_p + of * kWaves * 16 * ld_p, last_p * ld_p) : min(first_q + of * kWaves * 16 * ld_q, last_q * ld_q);
+            load_to_lds(p ? res_p : res_q, v + piece, k, base + slot + (u * kWaves + wave) * 1024);
         };
-        // codes past the contraction's end become zeros (in the last k-tile)
-        const int tail = g.K - (g.k_tiles - 1) * kBlock;
-        auto mend = [&](int turn, unsigned buffer) {
-            if (tail == kBlock || kt0 + turn != g.k_tiles - 1) return;
+        // codes past the contraction's end become zeros
+        auto mend = [&](int part, unsigned slot) {
+            const int there = g.K - kt0 * kBlock - part * 64;
+            if (there >= 64 || part >= parts) return;
             int first = t;
             asm volatile("" : "+v"(first));
-            for (int i = first; i < (BM + BN) * 8; i += kThreads) {
-                const int row = i / 8, p = i % 8;
-                v4u* at = reinterpret_cast<v4u*>(lds + buffer + row * kBlock + ((p ^ (row >> 1)) & 7) * 16);
-                if (p * 16 + 16 > tail) {
-                    v4u v = *at;
-                    keep_codes(v, tail - p * 16);
-                    *at = v;
-                }
+            for (int i = first; i < (BM + BN) * 4; i += kThreads) {
+                const int row = i / 4, p = i % 4;
+                if (p * 16 + 16 <= there) continue;
+                v4u* at = reinterpret_cast<v4u*>(lds + slot + row * 64 + ((p ^ (row >> 2)) & 3) * 16);
+                v4u v = *at;
+                keep_codes(v, there - p * 16);
+                *at = v;
             }
-            wait_and_meet();
+            wait_and_meet<0>();
         };
-        // Scales: four k-tiles' of every row in LDS, loaded with the first of the four.  A row's of a matrix of tiles is its block's.
+        // Scales: four groups' of every row in LDS, loaded with the first of the four.  A row's of a matrix of tiles is its block's.
         const int scale_p0 = m0 >> g.p_shift, scale_q0 = n0 >> g.q_shift, four_bytes = (ceil_div(g.K, kBlock) + 3) / 4 * 4;
         const int scale_ld_p = (int)g.P.scale_ld, scale_ld_q = (int)g.Q.scale_ld;
         const v4i res_sp = resource_of(g.P.scales + (long long)scale_p0 * scale_ld_p, (((m0 + last_p) >> g.p_shift) - scale_p0) * scale_ld_p + four_bytes);
@@ -244,14 +245,13 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
 #pragma unroll
             for (int j = 0; j < NT; ++j) sq[j] = next_sq[j];
         };
-        // An operand of one step, 64 q: lane holds 32 q of row r32, pieces 4 step + 2 half and the next.  Read r of a step's.
-        const unsigned turn_p = (r32 >> 1) & 7, at_p = (wm + r32) * kBlock, at_q = (BM + wn + r32) * kBlock;
+        // An operand of a part: lane holds 32 q of row r32, pieces 2 half and the next.  Read r of a part's.
+        const unsigned place0 = ((2 * half) ^ ((r32 >> 2) & 3)) * 16, at_p = (wm + r32) * 64, at_q = (BM + wn + r32) * 64;
         v8i a[2][MT], q[2][NT];
-        auto read = [&](auto step, unsigned buffer, auto which) {
+        auto read = [&](auto set, unsigned slot, auto which) {
             constexpr int r = which(), i = r / 2, high = r % 2;
-            const unsigned place = (((4 * step() + 2 * half) ^ turn_p) ^ high) * 16;
-            const v4i x = *reinterpret_cast<const v4i*>(lds + buffer + (i < MT ? at_p : at_q) + place + 32 * (i < MT ? i : i - MT) * kBlock);
-            v8i& to = i < MT ? a[step()][i < MT ? i : 0] : q[step()][i < MT ? 0 : i - MT];
+            const v4i x = *reinterpret_cast<const v4i*>(lds + slot + (i < MT ? at_p : at_q) + (place0 ^ (high * 16)) + 32 * (i < MT ? i : i - MT) * 64);
+            v8i& to = i < MT ? a[set()][i < MT ? i : 0] : q[set()][i < MT ? 0 : i - MT];
 #pragma unroll
             for (int e = 0; e < 4; ++e) to[4 * high + e] = x[e];
         };
@@ -295,31 +295,24 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
         constexpr std::integral_constant<int, kLoads> loads;
         constexpr std::integral_constant<int, (kMfmas + 1) / 2> early;
         constexpr std::integral_constant<int, kMfmas - (kMfmas > 4 ? kMfmas / 4 : 1)> most;
-        // A k-tile is in LDS, the next on its way to the other half of it.  The barrier stands between a k-tile's two steps: by then
-        // every wave has the second step's operands in registers, the half is free for the k-tile after the next, and the next
-        // k-tile's first operands are read while the second step is multiplied.
+        // A part's operands are in registers, the next part is in LDS and two more are on their way.  At the barrier a part has been read
+        // by all, and the next one has come for all: the one after the next three goes where it lay.  (Past the last part the last is
+        // loaded again, and what lies in LDS read, which nothing looks at: a branch around a part of this would cost the sums a
+        // second set of registers.)
+        constexpr int kMeet = 2 * kLoads;
         request_scales(0);
-        if (((kt0 + 1) & 3) == 0) request_scales(1);
-        in_order<kLoads>([&](auto u) { request(0, 0, u); });
-        wait_and_meet();
+        if (((kt0 + 1) & 3) == 0 && turns > 1) request_scales(1);
+#pragma unroll
+        for (int part = 0; part < 4; ++part) in_order<kLoads>([&](auto u) { request(min(part, parts - 1), part * S::kPart, u); });
+        wait_and_meet<3 * kLoads>();
         mend(0, 0);
-        in_order<kLoads>([&](auto u) { request(min(1, turns - 1), S::kStage, u); });
         in_order<kScaleReads>([&](auto i) { read_scale(0, i); });
         in_order<kReads>([&](auto r) { read(s0, 0, r); });
-        unsigned buffer = 0;
-        for (int turn = 0; turn < turns; ++turn) {
-            asm volatile("" : "+v"(first_p), "+v"(first_q));
-            take_scales();
-            if constexpr (EXACT) {
-                in_order<kReads>([&](auto r) { read(s1, buffer, r); });
-                multiply_exactly(s0);
-            } else {
-                in_order<kMfmas>([&](auto f) {
-                    multiply(s0, f);
-                    share(reads, most, f, [&](auto from, auto count) { some(from, count, [&](auto r) { read(s1, buffer, r); }); });
-                });
-            }
-            // (the first step's multiplications stay on this side of the barrier)
+        const auto half_turn = [&](int part, auto set) {
+            constexpr std::integral_constant<int, 1 - set()> other;
+            const unsigned slot = (unsigned)(part & 3) * S::kPart, next = (unsigned)((part + 1) & 3) * S::kPart;
+            const int after = min(part + 4, parts - 1), turn = part / 2;
+            // (the multiplications before stay on that side of the barrier)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -327,28 +320,32 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
                     if constexpr (BM == 256) asm volatile("" : "+a"(acc[i][j]));
                     else asm volatile("" : "+v"(acc[i][j]));
                 }
-            wait_and_meet();
-            mend(turn + 1, buffer ^ S::kStage);
-            // (past the last k-tile the last is loaded again, and what lies in LDS read, which nothing looks at: a branch around a part of this
-            // would cost the sums a second set of registers)
-            const int after = min(turn + 2, turns - 1);
-            if (((kt0 + turn + 2) & 3) == 0) request_scales(after);
+            wait_and_meet<kMeet>();
+            mend(part + 1, next);
+            if (set() == 0) {
+                take_scales();
+                if (((kt0 + turn + 2) & 3) == 0) request_scales(min(turn + 2, turns - 1));
+            }
             if constexpr (EXACT) {
-                in_order<kLoads>([&](auto u) { request(after, buffer, u); });
-                in_order<kScaleReads>([&](auto i) { read_scale(turn + 1, i); });
-                in_order<kReads>([&](auto r) { read(s0, buffer ^ S::kStage, r); });
-                multiply_exactly(s1);
+                in_order<kLoads>([&](auto u) { request(after, slot, u); });
+                if (set() == 1) in_order<kScaleReads>([&](auto i) { read_scale(turn + 1, i); });
+                in_order<kReads>([&](auto r) { read(other, next, r); });
+                multiply_exactly(set);
             } else {
                 in_order<kMfmas>([&](auto f) {
-                    multiply(s1, f);
-                    share(loads, early, f, [&](auto from, auto count) { some(from, count, [&](auto u) { request(after, buffer, u); }); });
-                    share(scale_reads, early, f, [&](auto from, auto count) { some(from, count, [&](auto i) { read_scale(turn + 1, i); }); });
-                    share(reads, most, f, [&](auto from, auto count) { some(from, count, [&](auto r) { read(s0, buffer ^ S::kStage, r); }); });
+                    multiply(set, f);
+                    share(loads, early, f, [&](auto from, auto count) { some(from, count, [&](auto u) { request(after, slot, u); }); });
+                    if constexpr (set() == 1)
+                        share(scale_reads, early, f, [&](auto from, auto count) { some(from, count, [&](auto i) { read_scale(turn + 1, i); }); });
+                    share(reads, most, f, [&](auto from, auto count) { some(from, count, [&](auto r) { read(other, next, r); }); });
                 });
             }
-            buffer ^= S::kStage;
+        };
+        for (int part = 0; part < parts; part += 2) {
+            half_turn(part, s0);
+            half_turn(part + 1, s1);
         }
-        wait_and_meet();          // LDS becomes the epilogue's
+        wait_and_meet<0>();          // LDS becomes the epilogue's
     }
 
     // Accumulator element e of lane (r32, half) of square (i, j) is C[.. 32 i + 8 (e / 4) + 4 half + e % 4][.. 32 j + r32].  Rows turn through LDS, 16 of
@@ -383,9 +380,29 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
 }
 
 template <int BM, int BN, int WM, int WN, bool EXACT>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(BM == 256 ? 1 : 2, BM == 256 ? 1 : 2))) void k_block_product(const Args g) {
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_block_product(const Args g) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[Shape<BM, BN, WM, WN>::kBytes];
     product_tile<BM, BN, WM, WN, EXACT>(g, blockIdx.x, lds);
+}
+
+// Sums over rows of a few partial sums, a thread a column.
+constexpr int kSumCols = 256;
+__device__ __forceinline__ void sum_columns(const ColumnSums& a, unsigned block) {
+    const int col = block * kSumCols + threadIdx.x;
+    if (col >= a.cols) return;
+    float v = 0.0f;
+#pragma unroll 8
+    for (int p = 0; p < a.partials; ++p) v += a.partial[(size_t)p * a.cols + col];
+    a.out[col] = v;
+}
+// Both products of a backward pass in one launch, and what is left to do for db: the first `first` workgroups take dx, those up to `all`
+// dw, and the others db, which waits for neither.
+template <int BM, int BN, int WM, int WN, bool EXACT>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_block_both(const Args dx, const Args dw, unsigned first, unsigned all, const ColumnSums db) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[Shape<BM, BN, WM, WN>::kBytes];
+    if (blockIdx.x < first) product_tile<BM, BN, WM, WN, EXACT>(dx, blockIdx.x, lds);
+    else if (blockIdx.x < all) product_tile<BM, BN, WM, WN, EXACT>(dw, blockIdx.x - first, lds);
+    else sum_columns(db, blockIdx.x - all);
 }
 
 // Sums of the splits' partial sums, in their order, and what follows.
@@ -432,53 +449,82 @@ __global__ __launch_bounds__(kFinishThreads) void k_block_join(const Join x, uns
 // ================================================================================================
 // Up to 16 MT rows: the product is the reading of Q.  A workgroup takes 16 outputs, each of its waves every kFewWaves-th group of 128 of the
 // contraction: a lane has 2 x 16 bytes of its output's row (and of its sample's), which the matrix instruction takes as they come, for
-// operands of one order of q on both sides.  P may be dense: its group is put into 8 bits in registers, the four lanes that
-// hold a row's group finding its scale.
-constexpr int kFewWaves = 8, kFewOutputs = 16;
+// operands of one order of q on both sides.  All loads of `some` groups are under way at once, without a branch: past the last
+// group it is loaded again, and its codes made zeros.  P may be dense (of rows of eight values at least): its group is put into
+// 8 bits in registers, the four lanes that hold a row's group finding its scale.
+constexpr int kFewWaves = 8, kFewOutputs = 16, kFewLeast = 8;
+template <int XK> struct FewRow { Chunk<XK> c[4]; };
+template <> struct FewRow<E4M3_128> { v4u x, y; int byte; };
+
+// (there: columns from the group's first on to the row's end, which may be none)
+__device__ __forceinline__ v8i codes_there(v4u x, v4u y, int quarter, int there) {
+    if (there < kBlock) {
+        keep_codes(x, there - quarter * 16);
+        keep_codes(y, there - 64 - quarter * 16);
+    }
+    return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+}
 template <int XK>
-__device__ __forceinline__ v8i few_operand(const Mat& m, long long row, int k, int half16, int there, int& byte) {
+__device__ __forceinline__ void few_request(FewRow<XK>& r, const Mat& m, long long row, int k, int quarter, int K) {
     if constexpr (XK == E4M3_128) {
-        const uint8_t* p = (const uint8_t*)m.p + row * m.ld + (long long)k * kBlock + half16 * 16;
-        v4u x = *as_global<const v4u>(p), y = *as_global<const v4u>(p + 64);
-        byte = *as_global<const uint8_t>(m.scales + row * m.scale_ld + k);
-        if (there < kBlock) {
-            keep_codes(x, there - half16 * 16);
-            keep_codes(y, there - 64 - half16 * 16);
-        }
-        return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        const uint8_t* p = (const uint8_t*)m.p + row * m.ld + (long long)k * kBlock + quarter * 16;
+        r.x = *as_global<const v4u>(p);
+        r.y = *as_global<const v4u>(p + 64);
+        r.byte = *as_global<const uint8_t>(m.scales + row * m.scale_ld + k);
     } else {
-        typedef typename Stored<XK>::type T;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) fetch_chunk<XK, false>(r.c[h], m, row, k * kBlock + h / 2 * 64 + quarter * 16 + h % 2 * 8, K);
+    }
+}
+template <int XK>
+__device__ __forceinline__ v8i few_operand(const FewRow<XK>& r, int quarter, int there, int& byte) {
+    if constexpr (XK == E4M3_128) {
+        byte = r.byte;
+        return codes_there(r.x, r.y, quarter, there);
+    } else {
         float v[4][8];
-        const T* p = (const T*)m.p + row * m.ld + (long long)k * kBlock;
         unsigned top = 0;
-        bool odd = false;
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            const int col = h / 2 * 64 + half16 * 16 + h % 2 * 8;
-            load_values(p + col, min(max(there - col, 0), kChunk), v[h]);
+            take_chunk<XK, false>(r.c[h], there - (h / 2 * 64 + quarter * 16 + h % 2 * 8), v[h]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const unsigned b = __float_as_uint(finite_magnitude(v[h][i]));
-                odd |= !(fabsf(v[h][i]) < __builtin_inff());
-                top = max(top, b);
-            }
+            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[h][i]) & 0x7FFFFFFFu);
         }
-        top = max(top, (unsigned)__shfl_xor((int)top, 16));
-        top = max(top, (unsigned)__shfl_xor((int)top, 32));
-        byte = scale_byte(__uint_as_float(top));
-        const float inverse = scale_power(254 - byte), most = byte == kLargestScale ? 240.0f : 448.0f;
+        const auto of_row = [](unsigned m) {
+            m = max(m, (unsigned)__shfl_xor((int)m, 16));
+            return max(m, (unsigned)__shfl_xor((int)m, 32));
+        };
+        byte = scale_byte(__uint_as_float(of_row(top)));
         v8i out;
+        if (byte < kLargestScale) {
+            const float inverse = scale_power(254 - byte);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            float s[8];
+            for (int h = 0; h < 4; ++h) {
+                float s[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                s[i] = fminf(fmaxf(v[h][i] * inverse, -most), most);
-                if (odd) s[i] = fabsf(v[h][i]) < __builtin_inff() ? s[i] : __builtin_nanf("");
+                for (int i = 0; i < 8; ++i) s[i] = v[h][i] * inverse;
+                const v2u w = convert_eight(s);
+                out[2 * h] = (int)w[0];
+                out[2 * h + 1] = (int)w[1];
             }
-            const v2u w = convert_eight(s);
-            out[2 * h] = (int)w[0];
-            out[2 * h + 1] = (int)w[1];
+        } else {                              // (the four lanes of a row agree)
+            unsigned finite = 0;
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) finite = max(finite, __float_as_uint(finite_magnitude(v[h][i])));
+            byte = scale_byte(__uint_as_float(of_row(finite)));
+            const float inverse = scale_power(254 - byte), most = byte == kLargestScale ? 240.0f : 448.0f;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                float s[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    s[i] = fabsf(v[h][i]) < __builtin_inff() ? fminf(fmaxf(v[h][i] * inverse, -most), most) : __builtin_nanf("");
+                const v2u w = convert_eight(s);
+                out[2 * h] = (int)w[0];
+                out[2 * h + 1] = (int)w[1];
+            }
         }
         return out;
     }
@@ -486,45 +532,49 @@ __device__ __forceinline__ v8i few_operand(const Mat& m, long long row, int k, i
 
 template <int XK, int MT, bool EXACT>
 __global__ __launch_bounds__(64 * kFewWaves) void k_block_few(const Args g) {
+    constexpr int kSome = XK == F32 || MT > 1 ? 2 : 4;
     __shared__ float sums[kFewWaves][16 * MT][kFewOutputs + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, quarter = lane >> 4;
     const int n0 = blockIdx.x * kFewOutputs, n = min(n0 + r16, g.N - 1);
     v4f acc[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const uint8_t* q_row = (const uint8_t*)g.Q.p + (long long)n * g.Q.ld + quarter * 16;
-    const uint8_t* q_scales = g.Q.scales + (long long)(n >> g.q_shift) * g.Q.scale_ld;
-    const auto group = [&](int k) {
-        const int there = min(g.K - k * kBlock, kBlock);
-        v4u x = *as_global<const v4u>(q_row + (long long)k * kBlock), y = *as_global<const v4u>(q_row + (long long)k * kBlock + 64);
-        const int q_byte = *as_global<const uint8_t>(q_scales + k);
-        if (there < kBlock) {
-            keep_codes(x, there - quarter * 16);
-            keep_codes(y, there - 64 - quarter * 16);
+    const uint8_t* const q_scales = g.Q.scales + (long long)(n >> g.q_shift) * g.Q.scale_ld;
+    const uint8_t* const q_row = (const uint8_t*)g.Q.p + (long long)n * g.Q.ld + quarter * 16;
+#pragma unroll 1
+    for (int k0 = wave; k0 < g.k_tiles; k0 += kSome * kFewWaves) {
+        FewRow<E4M3_128> q[kSome];
+        FewRow<XK> x[kSome][MT];
+#pragma unroll
+        for (int u = 0; u < kSome; ++u) {
+            const int k = min(k0 + u * kFewWaves, g.k_tiles - 1);
+            q[u].x = *as_global<const v4u>(q_row + (long long)k * kBlock);
+            q[u].y = *as_global<const v4u>(q_row + (long long)k * kBlock + 64);
+            q[u].byte = *as_global<const uint8_t>(q_scales + k);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) few_request<XK>(x[u][i], g.P, min(16 * i + r16, g.M - 1), k, quarter, g.K);
         }
-        const v8i b = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        v8bf values[4];
-        if constexpr (EXACT) values_of(b, q_byte, values);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            int byte;
-            const v8i a = few_operand<XK>(g.P, min(16 * i + r16, g.M - 1), k, quarter, there, byte);
-            if constexpr (EXACT) {
-                v8bf x[4];
-                values_of(a, byte, x);
+        for (int u = 0; u < kSome; ++u) {
+            const int there = g.K - (k0 + u * kFewWaves) * kBlock;
+            const v8i b = codes_there(q[u].x, q[u].y, quarter, there);
+            v8bf values[4];
+            if constexpr (EXACT) values_of(b, q[u].byte, values);
 #pragma unroll
-                for (int h = 0; h < 4; ++h) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[h], values[h], acc[i], 0, 0, 0);
-            } else {
-                acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[i], 0, 0, 0, byte, 0, q_byte);
+            for (int i = 0; i < MT; ++i) {
+                int byte;
+                const v8i a = few_operand<XK>(x[u][i], quarter, there, byte);
+                if constexpr (EXACT) {
+                    v8bf y[4];
+                    values_of(a, byte, y);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[h], values[h], acc[i], 0, 0, 0);
+                } else {
+                    acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[i], 0, 0, 0, byte, 0, q[u].byte);
+                }
             }
         }
-    };
-    int k = wave;
-    for (; k + 3 * kFewWaves < g.k_tiles; k += 4 * kFewWaves) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) group(k + u * kFewWaves);
     }
-    for (; k < g.k_tiles; k += kFewWaves) group(k);
     // element e of lane (r16, quarter): row 4 quarter + e, output r16
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -608,7 +658,7 @@ size_t block_product_scratch_bytes(int M, int N, int K) {
     return std::min((size_t)kGroups * 256 * 256, (size_t)splits * M * N) * sizeof(float);
 }
 
-bool block_product_takes_dense(int M, const Mat& y, const Mat& z) { return M <= kDenseRows && few_outputs(y, z); }
+bool block_product_takes_dense(int M, int K, const Mat& y, const Mat& z) { return M <= kDenseRows && K >= kFewLeast && few_outputs(y, z); }
 
 hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
     if (g.M <= kFewRows && few_outputs(g.f.y, g.f.z) && g.P.kind != E4M3_TILES) {
@@ -623,10 +673,10 @@ hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
     const Args a = args_of(g, p);
     const dim3 grid((unsigned)a.tiles_m * a.tiles_n * a.splits);
     if (exact(g.f)) {
-        if (p.tile == 256) k_block_product<256, 256, 2, 2, true><<<grid, 256, 0, s>>>(a);
+        if (p.tile == 256) k_block_product<256, 256, 4, 2, true><<<grid, 512, 0, s>>>(a);
         else k_block_product<128, 128, 2, 2, true><<<grid, 256, 0, s>>>(a);
     } else {
-        if (p.tile == 256) k_block_product<256, 256, 2, 2, false><<<grid, 256, 0, s>>>(a);
+        if (p.tile == 256) k_block_product<256, 256, 4, 2, false><<<grid, 512, 0, s>>>(a);
         else k_block_product<128, 128, 2, 2, false><<<grid, 256, 0, s>>>(a);
     }
     const hipError_t e = hipGetLastError();
@@ -634,9 +684,24 @@ hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
 }
 
 hipError_t launch_block_backward(const BlockProduct& dx, const BlockProduct& dw, const ColumnSums& db, hipStream_t s) {
+    const bool has_dx = dx.f.y.p && dx.M > 0, has_dw = dw.f.y.p;
+    if (has_dx && has_dw && exact(dx.f) == exact(dw.f)) {
+        // one tile for both, in one launch, unless apart they take less
+        const Plan px = plan_of(dx.M, dx.N, dx.K), pw = plan_of(dw.M, dw.N, dw.K);
+        const Plan x = plan_with(128, dx.M, dx.N, dx.K), w = plan_with(128, dw.M, dw.N, dw.K);
+        if (x.us + w.us < px.us + pw.us + 4.0) {
+            const Args ax = args_of(dx, x), aw = args_of(dw, w);
+            const unsigned first = (unsigned)ax.tiles_m * ax.tiles_n * ax.splits, all = first + (unsigned)aw.tiles_m * aw.tiles_n * aw.splits;
+            const unsigned sums = db.out ? (unsigned)ceil_div(db.cols, kSumCols) : 0;
+            if (exact(dx.f)) k_block_both<128, 128, 2, 2, true><<<dim3(all + sums), 256, 0, s>>>(ax, aw, first, all, db);
+            else k_block_both<128, 128, 2, 2, false><<<dim3(all + sums), 256, 0, s>>>(ax, aw, first, all, db);
+            const hipError_t e = hipGetLastError();
+            return e != hipSuccess ? e : finish(join_of(ax), join_of(aw), kNoSums, s);
+        }
+    }
     hipError_t e = finish(kNoJoin, kNoJoin, db, s);
-    if (e == hipSuccess && dx.f.y.p && dx.M > 0) e = launch_block_product(dx, s);
-    if (e == hipSuccess && dw.f.y.p) e = launch_block_product(dw, s);
+    if (e == hipSuccess && has_dx) e = launch_block_product(dx, s);
+    if (e == hipSuccess && has_dw) e = launch_block_product(dw, s);
     return e;
 }
 
