@@ -67,10 +67,10 @@ __device__ __forceinline__ void values(Chunk<F32>& c, float (&v)[8]) {
 }
 
 // A workgroup of THREADS walks rows; a thread holds NCH chunks of eight logits of one as they lie in memory (all of the row; AGAIN: rows that are
-// longer are read again for every pass).  With c = log2(e) / T and a shift b = most c, e^((z - most) / T) is 2^(z c - b), one fused
-// operation before the exponential: off by 2 |z c - b| 2^-24 of itself, which no sum feels, for where that is large the term is
-// small.  What the loss subtracts is subtracted in 64 bits: the difference of two logarithms that nearly agree is what a student
-// near its teacher has.
+// longer are read again for every pass).  e^((z - most) / T) is 2^((z - most) c) with c = log2(e) / T: off by 3 |(z - most) c| 2^-24 of itself,
+// which no sum feels, for where that is large the term is small.  (z c - most c in one fused operation would be an instruction less,
+// and nothing at all where logits are large: most c is rounded.)  What the loss subtracts is subtracted in 64 bits: the difference
+// of two logarithms that nearly agree is what a student near its teacher has.
 //
 // Entries: each of the teacher's is read once into LDS with the student's logit of its class, before anything is written (dlogits
 // may be the logits).  The gradient q T weight is written from the registers by whoever holds it; after a barrier the
@@ -175,7 +175,6 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BLOCKS 
         most = wave_most[0];
 #pragma unroll
         for (int i = 1; i < kWaves; ++i) most = fmaxf(most, wave_most[i]);
-        const float shift = most * c;
         float total = 0.0f;
         for (int turn = 0; turn < turns; ++turn) {
             if constexpr (AGAIN) {
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BLOCKS 
                 float v[8];
                 values(raw[j], v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) total += __builtin_amdgcn_exp2f(fmaf(v[i], c, -shift));
+                for (int i = 0; i < 8; ++i) total += __builtin_amdgcn_exp2f((v[i] - most) * c);
             }
         }
         total = wave_sum(total);
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BLOCKS 
         if (a.dlogits.p) {
             const float per = empty ? 0.0f : strange ? __builtin_nanf("") : scale / total;
             if (empty) write([&](float) { return 0.0f; });
-            else write([&](float v) { return __builtin_amdgcn_exp2f(fmaf(v, c, -shift)) * per; });
+            else write([&](float v) { return __builtin_amdgcn_exp2f((v - most) * c) * per; });
             // (the stores of all waves have arrived before any of an entry's is made)
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
@@ -234,7 +233,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BLOCKS 
                         p += p_of(e);
                     }
                     if (!first) continue;
-                    const float q = __builtin_amdgcn_exp2f(fmaf(entry_z[i], c, -shift)) / total;
+                    const float q = __builtin_amdgcn_exp2f((entry_z[i] - most) * c) / total;
                     *as_global<Value>((Value*)a.dlogits.p + row * a.dlogits.ld + k) = (Value)(scale * (q - p));
                 }
             }
@@ -243,9 +242,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BLOCKS 
         if (a.loss && wave == 0) {
             double sum = 0.0;
             if (!empty) {
-                // (total is of 2^(z c - shift), and shift is most c but for its rounding)
-                const double apart = log((double)total) - log((double)among) + ((double)shift - (double)most * (double)c) * 0.69314718055994531,
-                             per = 1.0 / (double)a.temperature;
+                const double apart = log((double)total) - log((double)among), per = 1.0 / (double)a.temperature;
 #pragma unroll 1
                 for (int i = lane; i < a.top; i += kWave) {
                     const float p = p_of(i);
