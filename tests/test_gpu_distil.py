@@ -54,6 +54,35 @@ def test_loss_and_gradient(rows, classes, top, dtype):
         assert torch.equal(d2, d) and (torch.equal(there, loss) if k != 1 else bool((there == MARK).all()))
 
 
+# every kernel for many rows, each with rows that end in its last chunks
+MANY = [7, 300, 513, 1024, 1025, 2047, 2049, 4095, 4100, 6145, 8191, 8200, 12289, 16380, 16385, 24577, 32767, 32770, 40961, 49153, 57345, 65535, 65544]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", MANY)
+def test_many_rows(classes, dtype):
+    """More rows than a workgroup each can be given at once.  (The reference runs on the GPU in 64 bits.)"""
+    rows, top, T = 600, min(classes, 70), 2.0
+    z = values(1, rows, classes, dtype=dtype, std=3.0) if classes < 3000 else None
+    if z is None:
+        g = torch.Generator(device=DEV)
+        g.manual_seed(classes)
+        z = torch.randn(rows, classes, generator=g, device=DEV).mul_(3).to(TYPE[dtype]).double()
+    z = z.to(DEV)
+    order = torch.stack([torch.randperm(classes, generator=torch.Generator().manual_seed(r))[:top] for r in range(rows)]).to(torch.int32).to(DEV)
+    t = (z.gather(1, order.long()) + values(2, rows, top).to(DEV)).float().double()
+    order[3] = order[3, 0]
+    order[5] = -1
+    weight = values(3, rows).abs().float().double().to(DEV)
+    weight[7] = 0
+    r = R.distil(z, t, order, T, weight)
+    p = P.Distillation(rows, classes, top, dtype, temperature=T)
+    loss = p.forward(z.to(TYPE[dtype]), t.float(), order, weight.float())
+    for name, got, (want, bound) in (("loss", loss, r["loss"]), ("dlogits", p.dlogits, r["dlogits"])):
+        off = (got.double() - want).abs()
+        assert bool((off <= bound + R.HALF[got.dtype] * (want.abs() + bound) + 1e-40).all()), name
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("classes, top", [(50, 6), (3000, 70), (140000, 6)])
 def test_rows_without_entries_weights_of_zero_and_repeated_classes(classes, top, dtype):
