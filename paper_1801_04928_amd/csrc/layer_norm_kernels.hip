@@ -164,6 +164,110 @@ struct Backward {
     float* partial;      // [gridDim.x][2][cols], or null
 };
 
+// The gradients of gain and shift for 64 columns, over all rows, by a whole block of THREADS: eight threads hold the columns' chunks, and every
+// THREADS / 8-th row is a thread's.  For few rows, whose dy and s are read once more for it: that costs less than another launch.
+constexpr int kStripCols = 64;
+template <int T, int S, int THREADS>
+__device__ __forceinline__ void strip_gradients(const Backward& a, float* dgain, float* dshift, int strip) {
+    constexpr int kWays = THREADS / 8, kWaves = THREADS / kWave, kSome = 4;
+    __shared__ float sums[kWaves][2][kStripCols];
+    const int col = strip * kStripCols + threadIdx.x % 8 * kChunk, n = min(max(a.cols - col, 0), kChunk);
+    float total[2][8] = {};
+#pragma unroll 1
+    for (int row0 = threadIdx.x / 8; row0 < a.rows; row0 += kWays * kSome) {
+        float dy[kSome][8], h[kSome][8], rstd[kSome], mean[kSome];
+#pragma unroll
+        for (int u = 0; u < kSome; ++u) {
+            const int row = row0 + u * kWays, there = row < a.rows ? n : 0;
+            load_chunk<T>(a.dy, row, col, there, dy[u]);
+            load_chunk<S>(a.sum, row, col, there, h[u]);
+            rstd[u] = a.rstd[min(row, a.rows - 1)];
+            mean[u] = a.mean[min(row, a.rows - 1)];
+        }
+#pragma unroll
+        for (int u = 0; u < kSome; ++u) {
+            const bool there = row0 + u * kWays < a.rows;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // (what is not there has no part in it, whatever lies in the statistics that were read for it)
+                total[0][i] = fmaf(dy[u][i], there && i < n ? (h[u][i] - mean[u]) * rstd[u] : 0.0f, total[0][i]);
+                total[1][i] += dy[u][i];
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float v = total[k][i];
+            v += __shfl_xor(v, 8);
+            v += __shfl_xor(v, 16);
+            v += __shfl_xor(v, 32);
+            if (threadIdx.x % kWave < 8) sums[threadIdx.x / kWave][k][threadIdx.x % 8 * kChunk + i] = v;
+        }
+    __syncthreads();
+    if (threadIdx.x >= 2 * kStripCols) return;
+    const int k = threadIdx.x / kStripCols, c = threadIdx.x % kStripCols, at = strip * kStripCols + c;
+    float v = sums[0][k][c];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v += sums[w][k][c];
+    float* const out = k == 0 ? dgain : dshift;
+    if (out && at < a.cols) out[at] = v;
+}
+
+// A few rows: a row at a time and no sums over them, which blocks of their own take at the same time (strip_gradients).
+template <int T, int S, int TPR, int NCH, bool NARROW>
+__global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_layer_backward_few(const Backward a, int row_blocks, float* dgain, float* dshift) {
+    constexpr int kBlockThreads = TPR > kThreads ? TPR : kThreads, kRows = kBlockThreads / TPR;
+    if ((int)blockIdx.x >= row_blocks) {
+        strip_gradients<T, S, kBlockThreads>(a, dgain, dshift, (int)blockIdx.x - row_blocks);
+        return;
+    }
+    __shared__ float shared[2][2][TPR > kWave ? TPR / kWave : 1];
+    int place = 0;
+    const int t = threadIdx.x % TPR, mine = kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    const long long row = (long long)blockIdx.x * kRows + mine;
+    if (row >= a.rows) return;                              // (with several rows a block there is no barrier)
+    const bool more = a.dsum.p != nullptr;
+    const auto col_of = [&](int j) { return (j * TPR + t) * kChunk; };
+    Chunk<T> dy_raw[NCH], dsum_raw[NCH];
+    Chunk<S> s_raw[NCH];
+    const float rstd = a.rstd[row], mean = a.mean[row];
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        fetch_chunk<T, NARROW>(dy_raw[j], a.dy, row, col_of(j), a.cols);
+        fetch_chunk<S, NARROW>(s_raw[j], a.sum, row, col_of(j), a.cols);
+        if (more) fetch_chunk<T, NARROW>(dsum_raw[j], a.dsum, row, col_of(j), a.cols);
+    }
+    float dy[NCH][8], h[NCH][8], along[2] = {0.0f, 0.0f};      // sums of t h and of t
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        const int n = a.cols - col_of(j);
+        float g[8];
+        load_vector_of(a.gain, 1.0f, col_of(j), n, g);
+        take_chunk<T, NARROW>(dy_raw[j], n, dy[j]);
+        take_chunk<S, NARROW>(s_raw[j], n, h[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[j][i] = i < n ? (h[j][i] - mean) * rstd : 0.0f;
+            dy[j][i] *= g[i];
+            along[0] = fmaf(dy[j][i], h[j][i], along[0]);
+            along[1] += dy[j][i];
+        }
+    }
+    row_sums<TPR>(along, shared, place);
+    const float by = along[0] / (float)a.cols, level = along[1] / (float)a.cols;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        const int n = a.cols - col_of(j);
+        float d[8] = {};
+        if (more) take_chunk<T, NARROW>(dsum_raw[j], n, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, (dy[j][i] - level) - h[j][i] * by, d[i]);
+        store_chunk<T>(a.dx, row, col_of(j), n, d, n > 0);
+    }
+}
+
 // A block takes rows blockIdx.x, + gridDim.x, ...: the sums of dy h and of dy over its rows stay in registers, two rows of partial
 // sums a block are all that both gradients cost in memory.  The next row is under way, as it lies in memory, while one is worked
 // on.  AGAIN as in the forward pass (the two gradients are then a kernel of their own, k_layer_gradients).
@@ -409,16 +513,39 @@ template <int T>
 hipError_t forward_of(const Forward& a, hipStream_t s) {
     return a.y.kind == E4M3 ? forward<T, E4M3>(a, s) : a.y.kind == E4M3_128 ? forward<T, E4M3_128>(a, s) : forward<T, T>(a, s);
 }
+// 1024 threads have 128 registers each, which do not hold a row's two gradients beside the next row: of such rows the gradients are a
+// kernel of their own.  (16384 x 16384 bf16 in one, with 156 registers spilled: 1054 us.)
+constexpr int kThreadsWithSums = 512, kColsWithSums = 8192;
+// A few rows: the second reading of dy and s, of matrices that lie in the caches, costs less than the launch that ends partial sums.
+constexpr int kFewRows = 512;
+constexpr long long kFewElements = 8ll << 20;
+bool few(int rows, int cols) { return cols <= kHeldCols && rows <= kFewRows && (long long)rows * cols <= kFewElements; }
+
+template <int T, int S>
+hipError_t backward_few(const Backward& a, float* dgain, float* dshift, hipStream_t s) {
+    return by_width(a.cols, [&](auto tpr, auto nch, auto again, auto narrow) {
+        if constexpr (!again()) {
+            constexpr int block = tpr() > kThreads ? tpr() : kThreads;
+            const int rows = ceil_div(a.rows, block / tpr()), strips = dgain || dshift ? ceil_div(a.cols, kStripCols) : 0;
+            k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(rows + strips), block, 0, s>>>(a, rows, dgain, dshift);
+        }
+        return hipGetLastError();
+    });
+}
 template <int T, int S>
 hipError_t backward(const Backward& a, hipStream_t s) {
     return by_width(a.cols, [&](auto tpr, auto nch, auto again, auto narrow) {
         constexpr int block = tpr() > kThreads ? tpr() : kThreads;
-        const int groups = again() ? std::min(a.rows, kMostGroups) : layer_norm_partials(a.rows, a.cols);
-        k_layer_backward<T, S, tpr(), nch(), again(), narrow()><<<dim3(groups), block, 0, s>>>(a);
-        if (again() && a.partial) {
-            const int parts = layer_norm_partials(a.rows, a.cols);
-            k_layer_gradients<T, S><<<dim3(ceil_div(a.cols, kStripChunks * kChunk), parts), kThreads, 0, s>>>(a, ceil_div(a.rows, parts));
+        const int parts = layer_norm_partials(a.rows, a.cols);
+        if constexpr (again()) {
+            k_layer_backward<T, S, tpr(), nch(), true, narrow()><<<dim3(std::min(a.rows, kMostGroups)), block, 0, s>>>(a);
+        } else if constexpr (tpr() > kThreadsWithSums) {
+            k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(a.rows), block, 0, s>>>(a, a.rows, nullptr, nullptr);
+        } else {
+            k_layer_backward<T, S, tpr(), nch(), false, narrow()><<<dim3(parts), block, 0, s>>>(a);
         }
+        if (tpr() > kThreadsWithSums && a.partial)
+            k_layer_gradients<T, S><<<dim3(ceil_div(a.cols, kStripChunks * kChunk), parts), kThreads, 0, s>>>(a, ceil_div(a.rows, parts));
         return hipGetLastError();
     });
 }
@@ -433,8 +560,8 @@ hipError_t launch_layer_norm_forward(int rows, int cols, const Mat& x, const Mat
 }
 
 int layer_norm_partials(int rows, int cols) {
-    if (rows == 0) return 0;
-    if (cols > kHeldCols) return std::min(ceil_div(rows, 16), 64);
+    if (rows == 0 || few(rows, cols)) return 0;
+    if (cols > kColsWithSums) return std::min(ceil_div(rows, 16), 64);
     return std::min(ceil_div(rows, rows_per_block(cols)), 512);
 }
 
@@ -444,6 +571,10 @@ hipError_t launch_layer_norm_backward(int rows, int cols, const Mat& dy, const M
     if (rows > 0) {
         const Backward a{rows, cols, dy, sum, dsum, dx, gain, mean, rstd, dgain || dshift ? partial : nullptr};
         hipError_t e;
+        if (few(rows, cols)) {
+            if (dy.kind == F32) return sum.kind == E4M3 ? backward_few<F32, E4M3>(a, dgain, dshift, s) : backward_few<F32, F32>(a, dgain, dshift, s);
+            return sum.kind == E4M3 ? backward_few<BF16, E4M3>(a, dgain, dshift, s) : backward_few<BF16, BF16>(a, dgain, dshift, s);
+        }
         if (dy.kind == F32) e = sum.kind == E4M3 ? backward<F32, E4M3>(a, s) : backward<F32, F32>(a, s);
         else e = sum.kind == E4M3 ? backward<BF16, E4M3>(a, s) : backward<BF16, BF16>(a, s);
         if (e != hipSuccess) return e;

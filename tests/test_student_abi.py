@@ -31,7 +31,7 @@ def test_layer_norm_forward_refusals(change):
     assert "lf_layer_norm_forward" in P.lf_operator_error()
 
 
-def norm_back(rows=4, cols=40, dy=mat(B, 40), total=mat(B, 40), gain=FAKE, mean=FAKE, rstd=FAKE, dsum=None, dx=mat(B, 40), dgain=FAKE,
+def norm_back(rows=2000, cols=40, dy=mat(B, 40), total=mat(B, 40), gain=FAKE, mean=FAKE, rstd=FAKE, dsum=None, dx=mat(B, 40), dgain=FAKE,
               dshift=FAKE, workspace=FAKE, nbytes=1 << 20):
     return P.lf_layer_norm_backward(rows, cols, dy, total, gain, mean, rstd, dsum, dx, dgain, dshift, workspace, nbytes)
 
