@@ -4,16 +4,15 @@
 #include "chunks.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lf {
 namespace ops {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int NONE_KIND = -1;                             // no z
-constexpr int kHigh = 8;                                   // rows of a thread, below each other
+constexpr int NONE_KIND = -1;                              // no z
 constexpr int kAcross = kBlock / kChunk;                   // threads along a row
-static_assert(kAcross * kBlock / kHigh == kThreads, "the threads hold 128 x 128 values");
+constexpr int kLoadThreads = 256;
 
 __host__ __device__ constexpr int ceil_div(int a, int b) { return a / b + (a % b != 0); }
 
@@ -32,7 +31,6 @@ __device__ __forceinline__ void times_slope(int act, float (&d)[8], const float 
     }
 }
 
-__device__ __forceinline__ unsigned finite_bits(float v) { return __float_as_uint(finite_magnitude(v)); }
 // v / 2^(byte - 127) as the conversion takes it where a group holds what is not finite, which becomes NaN, or has the largest scale, of
 // which it holds at most 240 (256 would be no finite number).
 __device__ __forceinline__ float scaled(float v, int byte) {
@@ -40,67 +38,81 @@ __device__ __forceinline__ float scaled(float v, int byte) {
     return fabsf(v) < __builtin_inff() ? fminf(fmaxf(a, -most), most) : __builtin_nanf("");
 }
 
-// A workgroup keeps a block of 128 x 128 values in registers, thread t eight rows (8 (t / 16) and on) of eight columns (8 (t % 16) and
-// on).  A row's group is 16 lanes' chunks, so its scale is a maximum over a row of lanes; a column's is one over the thread's
-// eight rows, then over the 16 threads below each other, through LDS, which also turns the transposed codes: 128 bytes of a
-// column, whose 8-byte pieces lie at place p ^ (column / 8 % 16), so that the 16 threads of a row write to different banks.
-// TILES: one scale for all.  Bound by memory.
-template <int T, int Z, bool TILES>
-__global__ __launch_bounds__(kThreads) void k_block_save(const BlockSave a, int blocks_x) {
-    __shared__ unsigned tops[kThreads / kAcross][kBlock];
-    __shared__ float sums[kThreads / kAcross][kBlock];
+// m or the larger of |a| and |b|; a NaN stays one.
+__device__ __forceinline__ float largest_of(float m, float a, float b) {
+    float r;
+    asm("v_maximum3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(m), "v"(a), "v"(b));
+    return r;
+}
+
+// A workgroup keeps a block of 128 x 128 values in registers, thread t HIGH rows (HIGH (t / 16) and on) of eight columns (8 (t % 16) and on).  A
+// row's group is 16 lanes' chunks, so its scale is a maximum over a row of lanes; a column's is one over the thread's rows, then over
+// the threads below each other, through LDS, which also turns the transposed codes: 128 bytes of a column in pieces of HIGH, which
+// lie where the threads of a row write to different banks.  TILES: one scale for all.
+// HIGH = 8, 256 threads, where there are blocks enough: every value costs some thirty instructions, half of them the slope's, so the
+// time is memory's where four blocks a compute unit overlap what they load and what they compute.  HIGH = 4, 512 threads, for a few blocks.
+template <int T, int Z, bool TILES, int HIGH>
+__global__ __launch_bounds__(kAcross * kBlock / HIGH) __attribute__((amdgpu_waves_per_eu(4))) void k_block_save(const BlockSave a, int blocks_x) {
+    constexpr int kDown = kBlock / HIGH, kThreads = kAcross * kDown;
+    typedef typename std::conditional<HIGH == 8, v2u, unsigned>::type Piece;
+    __shared__ float tops[kDown][kBlock];
+    __shared__ float sums[kDown][kBlock];
     __shared__ uint8_t column_byte[kBlock];
     __shared__ __attribute__((aligned(16))) uint8_t turned[kBlock * kBlock];
     const int t = threadIdx.x, across = t % kAcross, down = t / kAcross;
     const int bx = (int)(blockIdx.x % (unsigned)blocks_x), by = (int)(blockIdx.x / (unsigned)blocks_x);
     const int c0 = bx * kBlock, r0 = by * kBlock;
-    const int col = c0 + across * kChunk, n = min(max(a.cols - col, 0), kChunk), row = r0 + down * kHigh;
+    const int col = c0 + across * kChunk, n = min(max(a.cols - col, 0), kChunk), row = r0 + down * HIGH;
 
-    float v[kHigh][8];
+    float v[HIGH][8];
 #pragma unroll
-    for (int i = 0; i < kHigh; ++i) load_chunk<T>(a.x, row + i, col, row + i < a.rows ? n : 0, v[i]);
-    if (Z != NONE_KIND) {
+    for (int i = 0; i < HIGH; ++i) load_chunk<T>(a.x, row + i, col, row + i < a.rows ? n : 0, v[i]);
+    if constexpr (Z != NONE_KIND) {
 #pragma unroll
-        for (int i = 0; i < kHigh; ++i) {
+        for (int i = 0; i < HIGH; ++i) {
             float z[8];
-            load_chunk<Z == NONE_KIND ? T : Z>(a.z, row + i, col, row + i < a.rows ? n : 0, z);
+            load_chunk<Z>(a.z, row + i, col, row + i < a.rows ? n : 0, z);
             times_slope(a.act, v[i], z);
         }
     }
     // largest magnitudes: of a row's group in `own`, of the thread's rows in each column; a value that is not finite shows in them
-    unsigned own[kHigh], down_top[8] = {};
+    float own[HIGH], down_top[8];
 #pragma unroll
-    for (int i = 0; i < kHigh; ++i) {
-        unsigned m = 0;
+    for (int i = 0; i < HIGH; ++i) {
+        own[i] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const unsigned b = __float_as_uint(v[i][j]) & 0x7FFFFFFFu;
-            m = max(m, b);
-            down_top[j] = max(down_top[j], b);
-        }
-        own[i] = m;
+        for (int j = 0; j < 8; j += 2) own[i] = largest_of(own[i], v[i][j], v[i][j + 1]);
     }
-    bool odd = false;
 #pragma unroll
-    for (int i = 0; i < kHigh; ++i) odd |= own[i] >= 0x7F800000u;
+    for (int j = 0; j < 8; ++j) {
+        down_top[j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < HIGH; i += 2) down_top[j] = largest_of(down_top[j], v[i][j], v[i + 1][j]);
+    }
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < HIGH; i += 2) most = largest_of(most, own[i], own[i + 1]);
+    const bool odd = !(most < __builtin_inff());
     if (odd) {                                             // what is not finite sets no scale
+        most = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) down_top[j] = 0;
+        for (int j = 0; j < 8; ++j) down_top[j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kHigh; ++i) {
-            own[i] = 0;
+        for (int i = 0; i < HIGH; ++i) {
+            own[i] = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const unsigned b = finite_bits(v[i][j]);
-                own[i] = max(own[i], b);
-                down_top[j] = max(down_top[j], b);
+                const float b = finite_magnitude(v[i][j]);
+                own[i] = fmaxf(own[i], b);
+                down_top[j] = fmaxf(down_top[j], b);
             }
+            most = fmaxf(most, own[i]);
         }
     }
     if (a.partial) {
         float s[8] = {};
 #pragma unroll
-        for (int i = 0; i < kHigh; ++i)
+        for (int i = 0; i < HIGH; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[j] += v[i][j];
 #pragma unroll
@@ -111,30 +123,27 @@ __global__ __launch_bounds__(kThreads) void k_block_save(const BlockSave a, int 
         for (int j = 0; j < 8; ++j) tops[down][across * kChunk + j] = down_top[j];
     }
     // (every value finite and no group of the largest scale: nothing to look at value by value)
-    unsigned most = 0;
-#pragma unroll
-    for (int i = 0; i < kHigh; ++i) most = max(most, own[i]);
-    const bool rare = __syncthreads_or(odd || scale_byte(__uint_as_float(most)) >= kLargestScale);
+    const bool rare = __syncthreads_or(odd || scale_byte(most) >= kLargestScale);
     int tile_byte = 0;
     if constexpr (TILES) {
-        unsigned m = 0;
-        for (int i = 0; i < kThreads / kAcross; ++i) m = max(m, tops[i][t % kBlock]);
-        m = sixteen_max(m);
+        float m = 0.0f;
+        for (int i = 0; i < kDown; ++i) m = fmaxf(m, tops[i][t % kBlock]);
+        m = __uint_as_float(sixteen_max(__float_as_uint(m)));
         __syncthreads();
         if (t % 16 == 0 && t < kBlock) tops[0][t / 16] = m;
         __syncthreads();
-        for (int i = 0; i < kBlock / 16; ++i) m = max(m, tops[0][i]);
-        tile_byte = scale_byte(__uint_as_float(m));
+        for (int i = 0; i < kBlock / 16; ++i) m = fmaxf(m, tops[0][i]);
+        tile_byte = scale_byte(m);
         if (t == 0) {
             if (a.out.p) *as_global<uint8_t>(a.out.scales + (long long)by * a.out.scale_ld + bx) = (uint8_t)tile_byte;
             if (a.out_t.p) *as_global<uint8_t>(a.out_t.scales + (long long)bx * a.out_t.scale_ld + by) = (uint8_t)tile_byte;
         }
     } else if (a.out_t.p) {
         if (t < kBlock) {
-            unsigned m = 0;
+            float m = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kThreads / kAcross; ++i) m = max(m, tops[i][t]);
-            const int byte = scale_byte(__uint_as_float(m));
+            for (int i = 0; i < kDown; ++i) m = fmaxf(m, tops[i][t]);
+            const int byte = scale_byte(m);
             column_byte[t] = (uint8_t)byte;
             if (c0 + t < a.cols) *as_global<uint8_t>(a.out_t.scales + (long long)(c0 + t) * a.out_t.scale_ld + by) = (uint8_t)byte;
         }
@@ -143,13 +152,13 @@ __global__ __launch_bounds__(kThreads) void k_block_save(const BlockSave a, int 
         const int c = t - (kThreads - kBlock);
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kThreads / kAcross; ++i) s += sums[i][c];
+        for (int i = 0; i < kDown; ++i) s += sums[i][c];
         if (c0 + c < a.cols) a.partial[(size_t)by * a.cols + c0 + c] = s;
     }
     if (a.out.p) {
 #pragma unroll
-        for (int i = 0; i < kHigh; ++i) {
-            const int byte = TILES ? tile_byte : scale_byte(__uint_as_float(sixteen_max(own[i])));
+        for (int i = 0; i < HIGH; ++i) {
+            const int byte = TILES ? tile_byte : scale_byte(__uint_as_float(sixteen_max(__float_as_uint(own[i]))));
             const float inverse = scale_power(254 - byte);
             float s[8];
 #pragma unroll
@@ -166,33 +175,43 @@ __global__ __launch_bounds__(kThreads) void k_block_save(const BlockSave a, int 
     }
     if (!a.out_t.p) return;
     __syncthreads();
+    // piece `down` of column c is at place down ^ across of 16, or of 32 at down ^ (4 across % 32): 16 bytes that belong together stay so
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int c = across * kChunk + j, byte = TILES ? tile_byte : column_byte[c];
         const float inverse = scale_power(254 - byte);
-        float s[8];
+        float s[8] = {};
 #pragma unroll
-        for (int i = 0; i < kHigh; ++i) s[i] = v[i][j] * inverse;
+        for (int i = 0; i < HIGH; ++i) s[i] = v[i][j] * inverse;
         if (rare) {
 #pragma unroll
-            for (int i = 0; i < kHigh; ++i) s[i] = scaled(v[i][j], byte);
+            for (int i = 0; i < HIGH; ++i) s[i] = scaled(v[i][j], byte);
         }
-        *reinterpret_cast<v2u*>(turned + c * kBlock + ((down ^ across) * 8)) = convert_eight(s);
+        const v2u codes = convert_eight(s);
+        Piece* const at = reinterpret_cast<Piece*>(turned + c * kBlock) + (HIGH == 8 ? down ^ across : down ^ (4 * across & 31));
+        if constexpr (HIGH == 8) *at = codes;
+        else *at = codes[0];
     }
     __syncthreads();
     for (int id = t; id < kBlock * kBlock / 16; id += kThreads) {
         const int c = id / 8, p = id % 8, turn = c / kChunk;
         if (c0 + c >= a.cols) break;
-        const v2u lo = *reinterpret_cast<const v2u*>(turned + c * kBlock + ((2 * p) ^ turn) * 8);
-        const v2u hi = *reinterpret_cast<const v2u*>(turned + c * kBlock + ((2 * p + 1) ^ turn) * 8);
-        *as_global<v4u>((uint8_t*)a.out_t.p + (long long)(c0 + c) * a.out_t.ld + r0 + p * 16) = v4u{lo[0], lo[1], hi[0], hi[1]};
+        v4u out;
+        if constexpr (HIGH == 8) {
+            const v2u lo = *reinterpret_cast<const v2u*>(turned + c * kBlock + ((2 * p) ^ turn) * 8);
+            const v2u hi = *reinterpret_cast<const v2u*>(turned + c * kBlock + ((2 * p + 1) ^ turn) * 8);
+            out = v4u{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            out = *reinterpret_cast<const v4u*>(turned + c * kBlock + (p ^ (turn & 7)) * 16);
+        }
+        *as_global<v4u>((uint8_t*)a.out_t.p + (long long)(c0 + c) * a.out_t.ld + r0 + p * 16) = out;
     }
 }
 
 // A thread takes a chunk of eight.
 template <int FROM, int TO>
-__global__ __launch_bounds__(kThreads) void k_block_load(int rows, int cols, const Mat from, const Mat to) {
-    const long long id = (long long)blockIdx.x * kThreads + threadIdx.x;
+__global__ __launch_bounds__(kLoadThreads) void k_block_load(int rows, int cols, const Mat from, const Mat to) {
+    const long long id = (long long)blockIdx.x * kLoadThreads + threadIdx.x;
     const int chunks = ceil_div(cols, kChunk), col = (int)(id % chunks) * kChunk, n = min(cols - col, kChunk);
     const long long row = id / chunks;
     if (row >= rows) return;
@@ -201,21 +220,29 @@ __global__ __launch_bounds__(kThreads) void k_block_load(int rows, int cols, con
     store_chunk<TO>(to, row, col, n, v, true);
 }
 
+constexpr long long kFewBlocks = 512;
 template <int T, int Z>
 void save(const BlockSave& a, hipStream_t s) {
     const int blocks_x = ceil_div(a.cols, kBlock);
-    const dim3 grid((unsigned)((long long)blocks_x * ceil_div(a.rows, kBlock)));
+    const long long blocks = (long long)blocks_x * ceil_div(a.rows, kBlock);
+    const dim3 grid((unsigned)blocks);
     const int type = a.out.p ? a.out.kind : a.out_t.kind;
-    if (type == E4M3_TILES) k_block_save<T, Z, true><<<grid, kThreads, 0, s>>>(a, blocks_x);
-    else k_block_save<T, Z, false><<<grid, kThreads, 0, s>>>(a, blocks_x);
+    constexpr int kMany = kAcross * kBlock / 8, kFew = kAcross * kBlock / 4;
+    if (blocks <= kFewBlocks) {
+        if (type == E4M3_TILES) k_block_save<T, Z, true, 4><<<grid, kFew, 0, s>>>(a, blocks_x);
+        else k_block_save<T, Z, false, 4><<<grid, kFew, 0, s>>>(a, blocks_x);
+    } else {
+        if (type == E4M3_TILES) k_block_save<T, Z, true, 8><<<grid, kMany, 0, s>>>(a, blocks_x);
+        else k_block_save<T, Z, false, 8><<<grid, kMany, 0, s>>>(a, blocks_x);
+    }
 }
 template <int FROM, int TO>
 hipError_t load(int rows, int cols, const Mat& in, const Mat& out, hipStream_t s) {
-    const long long blocks = ((long long)rows * ceil_div(cols, kChunk) + kThreads - 1) / kThreads;
+    const long long blocks = ((long long)rows * ceil_div(cols, kChunk) + kLoadThreads - 1) / kLoadThreads;
     // (a grid has fewer than 2^32 threads: rows are taken in parts)
-    const long long most = (1ll << 32) / kThreads - 1;
+    const long long most = (1ll << 32) / kLoadThreads - 1;
     if (blocks <= most) {
-        k_block_load<FROM, TO><<<dim3((unsigned)blocks), kThreads, 0, s>>>(rows, cols, in, out);
+        k_block_load<FROM, TO><<<dim3((unsigned)blocks), kLoadThreads, 0, s>>>(rows, cols, in, out);
         return hipGetLastError();
     }
     const int part = rows / 2 / kBlock * kBlock;
