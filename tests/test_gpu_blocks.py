@@ -64,7 +64,8 @@ def test_values_that_are_not_finite_and_the_largest(dtype):
 
 # (rows, outputs, inputs): few rows, in each number of 16 and past it; the tiles' ends in every direction; contractions that are split
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 333, 777), (2, 40, 7), (3, 129, 1300), (16, 50, 260), (17, 65, 300), (32, 31, 129), (33, 257, 90), (45, 130, 1083),
-         (64, 20, 2000), (65, 129, 70), (130, 260, 190), (128, 128, 128), (257, 140, 64), (300, 257, 259), (70, 30, 9000), (200, 333, 2600)]
+         (64, 20, 2000), (65, 129, 70), (130, 260, 190), (128, 128, 128), (257, 140, 64), (300, 257, 259), (70, 30, 9000), (200, 333, 2600),
+         (9, 40, 5200), (16, 20, 9000), (31, 33, 1900), (31, 33, 2100), (60, 18, 1000)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
