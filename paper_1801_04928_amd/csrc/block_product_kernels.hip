@@ -155,6 +155,15 @@ __device__ __forceinline__ void in_order(F&& f) {
     }
 }
 
+// f(from), f(from + 1), ... `count` of them.
+template <class FROM, class COUNT, class F>
+__device__ __forceinline__ void some(FROM, COUNT, F&& f) {
+    if constexpr (COUNT::value > 0) {
+        f(FROM());
+        some(std::integral_constant<int, FROM::value + 1>(), std::integral_constant<int, COUNT::value - 1>(), f);
+    }
+}
+
 // 64 q of a tile in LDS, a part: rows of 64 bytes, four pieces of 16, piece p of row i at place p ^ (i / 4 % 4), so that the pieces of 16
 // rows, which LDS serves at once, lie in different banks.  The load to LDS puts lane after lane, so a lane asks for the piece that
 // belongs to its place.  Rows past the operand's last are the last again, which nothing looks at.
@@ -286,15 +295,6 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
             constexpr int N = n(), W = window(), F = f(), from = F < W ? N * F / W : N, to = F < W ? N * (F + 1) / W : N;
             one(std::integral_constant<int, from>(), std::integral_constant<int, to - from>());
         };
-        const auto some = [](auto from, auto count, auto&& f) {
-            constexpr int FROM = from(), COUNT = count();
-            if constexpr (COUNT > 0) f(std::integral_constant<int, FROM>());
-            if constexpr (COUNT > 1) f(std::integral_constant<int, FROM + 1>());
-            if constexpr (COUNT > 2) f(std::integral_constant<int, FROM + 2>());
-            if constexpr (COUNT > 3) f(std::integral_constant<int, FROM + 3>());
-            if constexpr (COUNT > 4) f(std::integral_constant<int, FROM + 4>());
-            static_assert(COUNT <= 5);
-        };
         constexpr std::integral_constant<int, kReads> reads;
         constexpr std::integral_constant<int, kScaleReads> scale_reads;
         constexpr std::integral_constant<int, kLoads> loads;
@@ -387,13 +387,13 @@ __device__ __forceinline__ void product_tile(const Args& g, unsigned block, uint
 }
 
 template <int BM, int BN, int WM, int WN, bool EXACT>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_block_product(const Args g) {
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(BM == 256 ? 2 : 4, BM == 256 ? 2 : 4))) void k_block_product(const Args g) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[Shape<BM, BN, WM, WN>::kBytes];
     product_tile<BM, BN, WM, WN, EXACT>(g, blockIdx.x, lds);
 }
 
 // Sums over rows of a few partial sums, a thread a column.
-constexpr int kSumCols = 256;
+constexpr int kSumCols = 512;               // (as many as k_block_both has threads)
 __device__ __forceinline__ void sum_columns(const ColumnSums& a, unsigned block) {
     const int col = block * kSumCols + threadIdx.x;
     if (col >= a.cols) return;
@@ -405,7 +405,7 @@ __device__ __forceinline__ void sum_columns(const ColumnSums& a, unsigned block)
 // Both products of a backward pass in one launch, and what is left to do for db: the first `first` workgroups take dx, those up to `all`
 // dw, and the others db, which waits for neither.
 template <int BM, int BN, int WM, int WN, bool EXACT>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_block_both(const Args dx, const Args dw, unsigned first, unsigned all, const ColumnSums db) {
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_block_both(const Args dx, const Args dw, unsigned first, unsigned all, const ColumnSums db) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[Shape<BM, BN, WM, WN>::kBytes];
     if (blockIdx.x < first) product_tile<BM, BN, WM, WN, EXACT>(dx, blockIdx.x, lds);
     else if (blockIdx.x < all) product_tile<BM, BN, WM, WN, EXACT>(dw, blockIdx.x - first, lds);
@@ -805,10 +805,10 @@ hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
     const dim3 grid((unsigned)a.tiles_m * a.tiles_n * a.splits);
     if (exact(g.f)) {
         if (p.tile == 256) k_block_product<256, 256, 4, 2, true><<<grid, 512, 0, s>>>(a);
-        else k_block_product<128, 128, 2, 2, true><<<grid, 256, 0, s>>>(a);
+        else k_block_product<128, 128, 4, 2, true><<<grid, 512, 0, s>>>(a);
     } else {
         if (p.tile == 256) k_block_product<256, 256, 4, 2, false><<<grid, 512, 0, s>>>(a);
-        else k_block_product<128, 128, 2, 2, false><<<grid, 256, 0, s>>>(a);
+        else k_block_product<128, 128, 4, 2, false><<<grid, 512, 0, s>>>(a);
     }
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : finish(join_of(a), kNoJoin, kNoSums, s);
@@ -824,8 +824,8 @@ hipError_t launch_block_backward(const BlockProduct& dx, const BlockProduct& dw,
             const Args ax = args_of(dx, x), aw = args_of(dw, w);
             const unsigned first = (unsigned)ax.tiles_m * ax.tiles_n * ax.splits, all = first + (unsigned)aw.tiles_m * aw.tiles_n * aw.splits;
             const unsigned sums = db.out ? (unsigned)ceil_div(db.cols, kSumCols) : 0;
-            if (exact(dx.f)) k_block_both<128, 128, 2, 2, true><<<dim3(all + sums), 256, 0, s>>>(ax, aw, first, all, db);
-            else k_block_both<128, 128, 2, 2, false><<<dim3(all + sums), 256, 0, s>>>(ax, aw, first, all, db);
+            if (exact(dx.f)) k_block_both<128, 128, 4, 2, true><<<dim3(all + sums), 512, 0, s>>>(ax, aw, first, all, db);
+            else k_block_both<128, 128, 4, 2, false><<<dim3(all + sums), 512, 0, s>>>(ax, aw, first, all, db);
             const hipError_t e = hipGetLastError();
             return e != hipSuccess ? e : finish(join_of(ax), join_of(aw), kNoSums, s);
         }
