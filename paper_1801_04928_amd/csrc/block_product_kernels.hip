@@ -713,16 +713,22 @@ struct Plan {
 constexpr int kGroups = 256;             // workgroups that fill the chip
 constexpr int kLeastTiles = 2;           // of the contraction a split has
 
+// Measured: a tile of 128 x 128 takes 2.5 us for its start and end and 3.6 for each 1024 of the contraction where few of them run (128 x
+// 4096 x 4096: 17 us without the launch) and 5.1 where the chip is full of them (1024 x 4096 x 4096: 23); one of 256 x 256 10.5, and 8.5 to 12.2
+// (2048 x 2048 x 8192: 82, 4096 x 4096 x 8192: 108).  So the large win once they fill the chip (4096 x 4096 x 4096: 65 us against 94), the small
+// below (2048 x 2048 x 2048: 16 against 32).  What splits store and a launch reads again costs 2 us and 1 for each 4 MB.
 Plan plan_with(int tile, int M, int N, int K) {
-    const double start = tile == 128 ? 3.3 : 8.0, per_1024 = tile == 128 ? 4.0 : 13.0;
+    const double start = tile == 128 ? 2.5 : 10.5, alone = tile == 128 ? 3.6 : 8.5, crowded = tile == 128 ? 5.1 : 12.2;      // us, per 1024
     const int k_tiles = ceil_div(K, kBlock);
     const long long tiles = (long long)ceil_div(M, tile) * ceil_div(N, tile);
     const int most = (int)std::max<long long>(1, std::min<long long>(kGroups / tiles, k_tiles / kLeastTiles));
     Plan best{tile, 1, k_tiles, 1e300};
     for (int want = 1; want <= most; want = want < most && 2 * want > most ? most : 2 * want) {
         const int per = std::max(1, ceil_div(k_tiles, want)), splits = std::max(1, ceil_div(k_tiles, per));
-        double us = (double)((tiles * splits + kGroups - 1) / kGroups) * (start + per_1024 * per * kBlock / 1024);
-        if (splits > 1) us += 3.0 + (double)splits * M * N * 8 / 5e6;
+        const long long groups = tiles * splits;
+        const double per_1024 = alone + (crowded - alone) * std::min(1.0, (double)groups / kGroups);
+        double us = (double)((groups + kGroups - 1) / kGroups) * (start + per_1024 * per * kBlock / 1024);
+        if (splits > 1) us += 2.0 + (double)splits * M * N * 8 / 4e6;
         if (us < best.us) best = Plan{tile, splits, per, us};
     }
     return best;
