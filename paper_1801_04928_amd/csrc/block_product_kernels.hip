@@ -704,6 +704,7 @@ __global__ __launch_bounds__(64 * kStagedWaves) void k_block_few_staged(const Ar
 constexpr int kFewRows = 64;
 bool eight(const Mat& m) { return m.kind == E4M3_128; }      // (that a result is there is not needed for this)
 bool few_outputs(const Mat& y, const Mat& z) { return !eight(y) && !(z.p && eight(z)); }
+bool by_few(const BlockProduct& g) { return g.M <= kFewRows && few_outputs(g.f.y, g.f.z) && g.P.kind != E4M3_TILES; }
 
 // ---- which tiles ---------------------------------------------------------------------------------------------------------
 struct Plan {
@@ -736,6 +737,13 @@ Plan plan_with(int tile, int M, int N, int K) {
 Plan plan_of(int M, int N, int K) {
     const Plan small = plan_with(128, M, N, K), large = plan_with(256, M, N, K);
     return large.us < small.us ? large : small;
+}
+// Up to 64 rows may also go a workgroup for 16 outputs and all of the contraction (below the tiles' kernels).  Measured: 0.8 us and, for each 1024
+// of the contraction, 0.53 and 0.033 a row, for as many workgroups as fill the chip (8 x 4096 x 4096: 3.5 us against 8 by tiles; 64 x 4096 x 4096: 11.9
+// against 10.1; 64 x 8192 x 8192: 52 against 16).
+double few_us(int M, int N, int K) {
+    const int groups = ceil_div(N, kFewOutputs);
+    return ceil_div(groups, kGroups) * (0.8 + (0.53 + 0.033 * M) * ceil_div(K, kBlock) * kBlock / 1024);
 }
 
 Args args_of(const BlockProduct& g, const Plan& p) {
@@ -775,6 +783,7 @@ void few_staged(const Args& a, hipStream_t s) {
     else if (groups <= 256) k_block_few_staged<XK, 1, 256, EXACT><<<grid, threads, 0, s>>>(a);
     else k_block_few_staged<XK, 1, 512, EXACT><<<grid, threads, 0, s>>>(a);
 }
+constexpr double kSaveUs = 2.5;           // of a launch that puts a few rows into 8 bits
 // Whether a result shows what the instructions for 8 bits lose.
 bool exact(const Finish& f) { return f.y.kind == F32 || (f.z.p && f.z.kind == F32); }
 hipError_t finish(const Join& x, const Join& w, const ColumnSums& db, hipStream_t s) {
@@ -793,12 +802,14 @@ size_t block_product_scratch_bytes(int M, int N, int K) {
     return std::min((size_t)kGroups * 256 * 256, (size_t)splits * M * N) * sizeof(float);
 }
 
-bool block_product_takes_dense(int M, int K, const Mat& y, const Mat& z) {
-    return M <= kFewRows && K >= kFewLeast && (long long)M * ceil_div(K, kBlock) <= staged_groups(M) && few_outputs(y, z);
+bool block_product_takes_dense(int M, int N, int K, const Mat& y, const Mat& z) {
+    return M <= kFewRows && K >= kFewLeast && (long long)M * ceil_div(K, kBlock) <= staged_groups(M) && few_outputs(y, z) &&
+           few_us(M, N, K) < plan_of(M, N, K).us + kSaveUs;
 }
 
 hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
-    if (g.M <= kFewRows && few_outputs(g.f.y, g.f.z) && g.P.kind != E4M3_TILES) {
+    const Plan p = plan_of(g.M, g.N, g.K);
+    if (g.P.kind == F32 || g.P.kind == BF16 || (by_few(g) && few_us(g.M, g.N, g.K) < p.us)) {
         const Args a = args_of(g, Plan{128, 1, 1, 0});
         if (g.P.kind == F32) few_staged<F32, true>(a, s);      // (results have the storage type of a dense P)
         else if (g.P.kind == BF16) few_staged<BF16, false>(a, s);
@@ -806,7 +817,6 @@ hipError_t launch_block_product(const BlockProduct& g, hipStream_t s) {
         else few<false>(a, s);
         return hipGetLastError();
     }
-    const Plan p = plan_of(g.M, g.N, g.K);
     const Args a = args_of(g, p);
     const dim3 grid((unsigned)a.tiles_m * a.tiles_n * a.splits);
     if (exact(g.f)) {
@@ -826,7 +836,8 @@ hipError_t launch_block_backward(const BlockProduct& dx, const BlockProduct& dw,
         // one tile for both, in one launch, unless apart they take less
         const Plan px = plan_of(dx.M, dx.N, dx.K), pw = plan_of(dw.M, dw.N, dw.K);
         const Plan x = plan_with(128, dx.M, dx.N, dx.K), w = plan_with(128, dw.M, dw.N, dw.K);
-        if (x.us + w.us < px.us + pw.us + 4.0) {
+        const double x_us = by_few(dx) ? std::min(px.us, few_us(dx.M, dx.N, dx.K)) : px.us;
+        if (x.us + w.us < x_us + pw.us + 4.0) {
             const Args ax = args_of(dx, x), aw = args_of(dw, w);
             const unsigned first = (unsigned)ax.tiles_m * ax.tiles_n * ax.splits, all = first + (unsigned)aw.tiles_m * aw.tiles_n * aw.splits;
             const unsigned sums = db.out ? (unsigned)ceil_div(db.cols, kSumCols) : 0;

@@ -409,7 +409,7 @@ lf_status lf_block_linear_forward(int rows, int outputs, int inputs, const lf_ma
     uint8_t* const scratch = (uint8_t*)workspace;
     Mat p = mx;
     // (the products of a few rows take x as it is, and keep it in 8 bits in registers)
-    const bool made = dense && !lf::ops::block_product_takes_dense(rows, inputs, my, mz);
+    const bool made = dense && !lf::ops::block_product_takes_dense(rows, outputs, inputs, my, mz);
     if (made) p = Mat{scratch + at.x_off, at.x_ld, scratch + at.x_scales_off, at.x_scale_ld, LF_MATRIX_E4M3_128};
     if (made || mxt.p)
         LF_TRY(done(call, lf::ops::launch_block_save(lf::ops::BlockSave{rows, inputs, LF_ACT_NONE, mx, kAbsent, made ? p : kAbsent, mxt, nullptr}, s)));

@@ -96,7 +96,7 @@ struct BlockProduct {
     float* raw;
 };
 size_t block_product_scratch_bytes(int M, int N, int K);
-bool block_product_takes_dense(int M, int K, const Mat& y, const Mat& z);
+bool block_product_takes_dense(int M, int N, int K, const Mat& y, const Mat& z);
 hipError_t launch_block_product(const BlockProduct& g, hipStream_t s);
 // The two products of a backward pass, each with scratch of its own.
 hipError_t launch_block_backward(const BlockProduct& dx, const BlockProduct& dw, const ColumnSums& db, hipStream_t s);
