@@ -62,6 +62,22 @@ def test_values_that_are_not_finite_and_the_largest(dtype):
             same("codes", codes, want)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tiles", [False, True])
+def test_save_of_many_blocks(tiles, dtype):
+    rows, cols = 2050, 4300
+    x = spread(1, rows, cols, dtype)
+    mx, out, out_t = Dense(rows, cols, dtype, x, 1, 3), Blocks(rows, cols, tiles, pad_groups=1), Blocks(cols, rows, tiles)
+    assert P.lf_block_save(rows, cols, mx.m, out.m, out_t.m) == P.LF_OK
+    torch.cuda.synchronize()
+    for m, v in ((out, x), (out_t, x.t().contiguous())):
+        codes, e = m.raw()
+        want, want_e = (R.pack_tiles if tiles else R.pack)(v)
+        same("codes", codes, want)
+        same("scales", e, want_e)
+        del codes, e, want, want_e
+
+
 # (rows, outputs, inputs): few rows, in each number of 16 and past it; the tiles' ends in every direction; contractions that are split
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 333, 777), (2, 40, 7), (3, 129, 1300), (16, 50, 260), (17, 65, 300), (32, 31, 129), (33, 257, 90), (45, 130, 1083),
          (64, 20, 2000), (65, 129, 70), (130, 260, 190), (128, 128, 128), (257, 140, 64), (300, 257, 259), (70, 30, 9000), (200, 333, 2600),
@@ -135,6 +151,20 @@ def test_backward(rows, outputs, inputs, dtype):
         assert float(db[outputs]) == MARK
         if wanted[2]:
             near("db", db[:outputs], dz.sum(0), (rows + 40) * R.U * dz.abs().sum(0))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, outputs, inputs", [(64, 5003, 4100), (17, 8200, 2100), (5, 40, 40000), (2100, 4210, 1150), (2500, 2100, 1000), (3000, 3333, 130)])
+def test_forward_of_large_products(rows, outputs, inputs, dtype):
+    """Few rows whose products go by tiles, and tiles of every size with ends in every direction."""
+    x, w = values(1, rows, inputs, dtype=dtype), values(2, outputs, inputs, dtype=dtype, std=inputs ** -0.5)
+    bias = values(3, outputs, std=0.3)
+    p = P.BlockLinear(rows, outputs, inputs, dtype, act="silu", z=dtype, passes="forward")
+    p.set_params(w.to(TYPE[dtype]).to(DEV), bias.float().to(DEV))
+    p.forward(x.to(TYPE[dtype]).to(DEV))
+    (v, e_v), (want, e_y) = R.epilogue(*R.product(R.held(x), R.held_tiles(w), dtype == "f32"), bias, "silu", None)
+    near_rounded("z", p.z, v, e_v)
+    near_rounded("y", p.y, want, e_y)
 
 
 @pytest.mark.parametrize("act", ["sigmoid", "silu", "gelu"])

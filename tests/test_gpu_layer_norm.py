@@ -128,6 +128,29 @@ def test_backward_of_many_rows(rows, cols, dtype):
     near("dshift", n.dshift, *r["dshift"])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, cols", [(513, 5), (520, 700), (900, 70), (600, 9001)])
+def test_backward_of_many_rows_in_8_bits(rows, cols, dtype):
+    s, dy = values(1, rows, cols, dtype=dtype, mean=1), values(2, rows, cols, dtype=dtype, std=0.1)
+    ms, mdy, dx = Eight(rows, cols, s.numpy(), pad_groups=1), Dense(rows, cols, dtype, dy, 1, 2), Dense(rows, cols, dtype, None, 3, 1)
+    held = torch.from_numpy(from_eight(*to_eight(s.numpy())))
+    mean, rstd = held.mean(1).float(), (held - held.mean(1, keepdim=True)).square().mean(1).add(EPS).rsqrt().float()
+    dgain, dshift = (torch.full((cols + 1,), MARK, device=DEV) for _ in range(2))
+    gain, g = vector(4, cols, 1.0)
+    nbytes = P.lf_layer_norm_workspace_bytes(rows, cols)
+    scratch = torch.full((nbytes + 256,), 255, dtype=torch.uint8, device=DEV)
+    gmean, grstd = mean.to(DEV), rstd.to(DEV)
+    assert P.lf_layer_norm_backward(rows, cols, mdy.m, ms.m, g.data_ptr(), gmean.data_ptr(), grstd.data_ptr(), None, dx.m, dgain.data_ptr(),
+                                    dshift.data_ptr(), scratch.data_ptr(), nbytes) == P.LF_OK
+    torch.cuda.synchronize()
+    r = R.norm_backward(dy, held, gain, mean.double(), rstd.double(), None)
+    dx.get()
+    assert bool((scratch[nbytes:] == 255).all()) and float(dgain[cols]) == MARK and float(dshift[cols]) == MARK
+    near_rounded("dx", dx.t, *r["dx"])
+    near("dgain", dgain[:cols], *r["dgain"])
+    near("dshift", dshift[:cols], *r["dshift"])
+
+
 def test_outputs_in_the_inputs_place_and_fewer_rows():
     """sum may be x or branch, dx may be dsum; an object serves fewer rows than it was made for, and none."""
     x, branch = (values(i, 5, 70, dtype="bf16").bfloat16().to(DEV) for i in (1, 2))
