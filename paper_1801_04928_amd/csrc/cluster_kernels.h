@@ -303,6 +303,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_cluster(const Args g) {
     // ---- the waves that compute: units 4 s + wave of the contraction
     const __amdgpu_buffer_rsrc_t words = make_buffer(g.words, 2u * (unsigned)slices_all * (unsigned)g.units * 2048u);
     unsigned patience = g.patience;
+    // A forward pass that had no word to say so in (it allocates none under LF_SCHED_STREAMS) may have been lost: the chain's first
+    // launch says it, and not only where a wait of its own gives up.
+    if (BWD && g.y && g.lost_host && blockIdx.x == 0 && wave == 0 && lane == 0 && load_state(g.state + LOST))
+        __hip_atomic_store(g.lost_host, abort_code(g.layer, 0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
     __syncthreads();                                                        // the next numbers
     __syncthreads();                                                        // the first weights
     Task x = task(0);
