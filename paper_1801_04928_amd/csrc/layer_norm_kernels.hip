@@ -1,5 +1,6 @@
 // The layer norm with the residual's addition, and its backward pass.  Bound by memory: every value is read once, held in registers,
-// and written once.
+// and written once.  16384 x 8192 bf16, four matrices of it: forward 189 us, 5.7 TB/s, backward 199 us, 5.4 TB/s, where a copy of 1 GiB reaches
+// 5.1; small ones take the call's time on the host (1 x 1024 9 us, the kernel 3.4 of it).
 #include "chunks.h"
 #include "column_sums.h"
 
@@ -215,7 +216,8 @@ __device__ __forceinline__ void strip_gradients(const Backward& a, float* dgain,
     if (out && at < a.cols) out[at] = v;
 }
 
-// A few rows: a row at a time and no sums over them, which blocks of their own take at the same time (strip_gradients).
+// A few rows: a row at a time and no sums over them, which blocks of their own take at the same time (strip_gradients).  333 x 4100 fp32 10.5 us,
+// a load, a reduction and a store one after the other; with partial sums and a launch that ends them 17.
 template <int T, int S, int TPR, int NCH, bool NARROW>
 __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_layer_backward_few(const Backward a, int row_blocks, float* dgain, float* dshift) {
     constexpr int kBlockThreads = TPR > kThreads ? TPR : kThreads, kRows = kBlockThreads / TPR;
@@ -516,10 +518,10 @@ hipError_t forward_of(const Forward& a, hipStream_t s) {
 // 1024 threads have 128 registers each, which do not hold a row's two gradients beside the next row: of such rows the gradients are a
 // kernel of their own.  (16384 x 16384 bf16 in one, with 156 registers spilled: 1054 us.)
 constexpr int kThreadsWithSums = 512, kColsWithSums = 8192;
-// A few rows: the second reading of dy and s, of matrices that lie in the caches, costs less than the launch that ends partial sums.
-constexpr int kFewRows = 512;
-constexpr long long kFewElements = 8ll << 20;
-bool few(int rows, int cols) { return cols <= kHeldCols && rows <= kFewRows && (long long)rows * cols <= kFewElements; }
+// A few rows: the second reading of dy and s, of matrices that lie in the caches, costs less than the launch that ends partial sums (us, this
+// way | with partial sums: 256 x 1000 fp32 8.3 | 11.4, 500 x 8192 bf16 15.0 | 22.5, 512 x 16384 fp32 37 | 43).  Of s in 8 bits it takes longer, which shows
+// where a block has fewer than 512 threads: 256 x 1000 9.4 | 11.7, 400 x 1000 14.1 | 11.8.
+bool few(int rows, int cols, bool eight) { return cols <= kHeldCols && rows <= (eight && cols <= 4096 ? 256 : 512); }
 
 template <int T, int S>
 hipError_t backward_few(const Backward& a, float* dgain, float* dshift, hipStream_t s) {
@@ -560,7 +562,7 @@ hipError_t launch_layer_norm_forward(int rows, int cols, const Mat& x, const Mat
 }
 
 int layer_norm_partials(int rows, int cols) {
-    if (rows == 0 || few(rows, cols)) return 0;
+    if (rows == 0 || few(rows, cols, true)) return 0;         // (what any type needs)
     if (cols > kColsWithSums) return std::min(ceil_div(rows, 16), 64);
     return std::min(ceil_div(rows, rows_per_block(cols)), 512);
 }
@@ -571,7 +573,7 @@ hipError_t launch_layer_norm_backward(int rows, int cols, const Mat& dy, const M
     if (rows > 0) {
         const Backward a{rows, cols, dy, sum, dsum, dx, gain, mean, rstd, dgain || dshift ? partial : nullptr};
         hipError_t e;
-        if (few(rows, cols)) {
+        if (few(rows, cols, sum.kind == E4M3)) {
             if (dy.kind == F32) return sum.kind == E4M3 ? backward_few<F32, E4M3>(a, dgain, dshift, s) : backward_few<F32, F32>(a, dgain, dshift, s);
             return sum.kind == E4M3 ? backward_few<BF16, E4M3>(a, dgain, dshift, s) : backward_few<BF16, BF16>(a, dgain, dshift, s);
         }
