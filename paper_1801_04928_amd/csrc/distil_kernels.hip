@@ -1,5 +1,5 @@
 // The distillation loss from a teacher's top logits, and its gradient: softmax of a row of logits against a softmax of a few.  Bound by
-// memory: a row is read once, held in registers, and its gradient written once.  4096 x 64000 bf16 228 us, 4.6 TB/s: a workgroup loads, finds
+// memory: a row is read once, held in registers, and its gradient written once.  4096 x 64000 bf16 219 us, 4.8 TB/s: a workgroup loads, finds
 // the maximum, the sum, and stores, and two or three of them overlap on a compute unit.  Small ones are those steps' latencies: 32 x 1000 fp32 4.6 us.
 #include "chunks.h"
 
@@ -109,6 +109,9 @@ __device__ __forceinline__ void subtract(Chunk<F32>& c, float x) {
     for (int i = 0; i < 8; ++i) c.a[i / 4][i % 4] -= x;
 }
 
+typedef int v4i __attribute__((ext_vector_type(4)));
+__host__ __device__ constexpr int whole_fours(int n) { return (n + 3) / 4 * 4; }
+
 // A workgroup of THREADS walks rows; a thread holds NCH chunks of eight logits of one as they lie in memory (all of the row, whose chunks but
 // each thread's last NCH - WHOLE are whole; AGAIN: rows that are longer are read again for every pass).  With c = log2(e) / T and b = most c, rounded,
 // e^((z - most) / T) is 2^(z c - b) but for a factor that all share: one fused operation before the exponential, off by 3 |z c - b| 2^-24
@@ -126,10 +129,12 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
     constexpr int kWaves = THREADS / kWave, kWhole = WHOLE;
     __shared__ float wave_most[kWaves], wave_total[kWaves];
     __shared__ int wave_wrong[kWaves];
-    extern __shared__ float entries[];                     // [3][top]: the teacher's logit, the student's, the class (-1: none)
+    extern __shared__ __attribute__((aligned(16))) float entries[];        // [4][top in whole fours]: the teacher's logit, the student's, p, the class (-1: none)
     float* const entry_t = entries;
-    float* const entry_z = entries + a.top;
-    int* const entry_class = (int*)(entries + 2 * a.top);
+    const int fours = whole_fours(a.top);
+    float* const entry_z = entries + fours;
+    float* const entry_p = entries + 2 * fours;
+    int* const entry_class = (int*)(entries + 3 * fours);
     const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
     const float c = 1.44269504088896341f / a.temperature;
     typedef typename Stored<T>::type Value;
@@ -216,6 +221,10 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
         if constexpr (!AGAIN) load(0);
         const float first_z = student(first_k);
         if (t < a.top) keep(t, first_k, first_v, first_z);
+        if (t < fours - a.top) {                           // (entries of none)
+            entry_class[a.top + t] = -1;
+            entry_p[a.top + t] = 0.0f;
+        }
 #pragma unroll 1
         for (int i = t + THREADS; i < a.top; i += THREADS) {
             int k;
@@ -244,6 +253,24 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
             most = larger(most, wave_most[i]);
             any_wrong |= wave_wrong[i];
         }
+        // the teacher's softmax: every wave takes its sums for itself, and p of its entries for all
+        float top_most = -__builtin_inff(), among = 0.0f;
+        bool strange = any_wrong != 0;                     // (the largest leaves NaN out)
+#pragma unroll 1
+        for (int i = lane; i < a.top; i += kWave) {
+            const float v = entry_t[i];
+            top_most = larger(top_most, v);
+            strange |= v != v;
+        }
+        top_most = wave_max(top_most);
+        strange = __any(strange);
+        const bool empty = !strange && top_most == -__builtin_inff();
+#pragma unroll 1
+        for (int i = lane; i < a.top; i += kWave) among += __builtin_amdgcn_exp2f((entry_t[i] - top_most) * c);
+        among = wave_sum(among);
+        if (strange) among = __builtin_nanf("");
+#pragma unroll 1
+        for (int i = t; i < a.top; i += THREADS) entry_p[i] = __builtin_amdgcn_exp2f((entry_t[i] - top_most) * c) / among;
         const bool far = fabsf(most * c) >= 0x1p20f;       // (the whole workgroup's)
         const auto come_near = [&]() {
             if (far) {
@@ -275,29 +302,12 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
 #pragma unroll
         for (int i = 1; i < kWaves; ++i) total += wave_total[i];
 
-        // the teacher's softmax: every wave takes it for itself
-        float top_most = -__builtin_inff(), among = 0.0f;
-        bool strange = any_wrong != 0;                     // (the largest leaves NaN out)
-#pragma unroll 1
-        for (int i = lane; i < a.top; i += kWave) {
-            const float v = entry_t[i];
-            top_most = larger(top_most, v);
-            strange |= v != v;
-        }
-        top_most = wave_max(top_most);
-        strange = __any(strange);
-        const bool empty = !strange && top_most == -__builtin_inff();
         const float scale = weight * a.temperature;
         if (a.dlogits.p) {
             const float per = empty ? 0.0f : strange ? __builtin_nanf("") : scale / total;
             if (empty) write(come_near, [&](float) { return 0.0f; });
             else write(come_near, [&](float v) { return __builtin_amdgcn_exp2f(fmaf(v, c, -shift)) * per; });
         }
-#pragma unroll 1
-        for (int i = lane; i < a.top; i += kWave) among += __builtin_amdgcn_exp2f((entry_t[i] - top_most) * c);
-        among = wave_sum(among);
-        if (strange) among = __builtin_nanf("");
-        const auto p_of = [&](int i) { return __builtin_amdgcn_exp2f((entry_t[i] - top_most) * c) / among; };
         // (total is of 2^(z c - shift), and shift is most c but for its rounding, if it is not 0 with the largest subtracted)
         const double rounding = far ? 0.0 : (double)shift - (double)most * (double)c;
         if (a.loss && wave == kWaves - 1) {
@@ -306,7 +316,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
                 const double apart = log((double)total) - log((double)among) + rounding * 0.69314718055994531, per = 1.0 / (double)a.temperature;
 #pragma unroll 1
                 for (int i = lane; i < a.top; i += kWave) {
-                    const float p = p_of(i);
+                    const float p = entry_p[i];
                     // (an entry of p = 0 adds nothing, whatever the student's logit)
                     if (!(p == 0.0f))
                         sum += (double)p * ((((double)entry_t[i] - (double)top_most) - ((double)entry_z[i] - (double)most)) * per + apart);
@@ -322,11 +332,16 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
                 if (k < 0) return -1;
                 float p = 0.0f;
                 bool first = true;
-#pragma unroll 4
-                for (int e = 0; e < a.top; ++e) {
-                    if (entry_class[e] != k) continue;
-                    if (e < i) first = false;
-                    p += p_of(e);
+#pragma unroll 2
+                for (int e = 0; e < fours; e += 4) {
+                    const v4i classes = *reinterpret_cast<const v4i*>(entry_class + e);
+                    const v4f ps = *reinterpret_cast<const v4f*>(entry_p + e);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const bool same = classes[u] == k;
+                        p += same ? ps[u] : 0.0f;
+                        first &= !(same && e + u < i);
+                    }
                 }
                 const float x = far ? (entry_z[i] - most) * c : fmaf(entry_z[i], c, -shift);
                 value = scale * (__builtin_amdgcn_exp2f(x) / total - p);
@@ -357,12 +372,12 @@ hipError_t start(const Distil& a, hipStream_t s) {
     constexpr int kRegisters = NCH * (T == BF16 ? 4 : 8) + 60;          // what a thread needs, about: the compiler is held to it
     constexpr int kStep = THREADS > 256 ? THREADS / 256 : 1, kWavesWanted = std::max(1, std::min(8, 512 / kRegisters) / kStep) * kStep;
     k_distil<T, THREADS, NCH, NCH - REST, AGAIN, NARROW, kWavesWanted>
-        <<<dim3((unsigned)std::min(a.rows, kMostRowsAGrid)), THREADS, 3 * a.top * sizeof(float), s>>>(a);
+        <<<dim3((unsigned)std::min(a.rows, kMostRowsAGrid)), THREADS, 4 * whole_fours(a.top) * sizeof(float), s>>>(a);
     return hipGetLastError();
 }
 
 // A row by as few threads as hold it: what a thread needs beside its logits, some 50 registers, is the same for one chunk and for sixteen,
-// so more rows are under way at once (us, this way | by four times the threads: 16384 x 8000 bf16 110 | 159, 512 x 12000 10.7 | 14.1, 1024 x 20000 fp32 35
+// so more rows are under way at once (us, this way | by four times the threads: 16384 x 8000 bf16 98 | 150, 512 x 12000 10 | 13, 1024 x 20000 fp32 35
 // | 44; of 32 rows either is the call's time, 8).
 template <int T>
 hipError_t by_width(const Distil& a, hipStream_t s) {
