@@ -52,7 +52,8 @@ __device__ __forceinline__ float largest_of(float m, float a, float b) {
 // lie where the threads of a row write to different banks.  TILES: one scale for all.
 // HIGH = 8, 256 threads, where there are blocks enough: every value costs some thirty instructions, half of them the slope's, so the
 // time is memory's where four blocks a compute unit overlap what they load and what they compute.  HIGH = 4, 512 threads, for a few blocks.
-template <int T, int Z, bool TILES, int HIGH>
+// NARROW: of fewer than eight columns.
+template <int T, int Z, bool TILES, int HIGH, bool NARROW = false>
 __global__ __launch_bounds__(kAcross * kBlock / HIGH) __attribute__((amdgpu_waves_per_eu(4))) void k_block_save(const BlockSave a, int blocks_x) {
     constexpr int kDown = kBlock / HIGH, kThreads = kAcross * kDown;
     typedef typename std::conditional<HIGH == 8, v2u, unsigned>::type Piece;
@@ -66,15 +67,35 @@ __global__ __launch_bounds__(kAcross * kBlock / HIGH) __attribute__((amdgpu_wave
     const int col = c0 + across * kChunk, n = min(max(a.cols - col, 0), kChunk), row = r0 + down * HIGH;
 
     float v[HIGH][8];
+    const auto there = [&](int i) { return row + i < a.rows ? n : 0; };
+    if (row < a.rows && n > 0) {       // (all loads are under way at once: past the last row it is loaded again)
+        Chunk<T> raw[HIGH];
 #pragma unroll
-    for (int i = 0; i < HIGH; ++i) load_chunk<T>(a.x, row + i, col, row + i < a.rows ? n : 0, v[i]);
-    if constexpr (Z != NONE_KIND) {
+        for (int i = 0; i < HIGH; ++i) fetch_chunk<T, NARROW>(raw[i], a.x, min(row + i, a.rows - 1), col, a.cols);
+        if constexpr (Z != NONE_KIND) {
+            constexpr int kSome = T == F32 && HIGH == 8 ? 4 : HIGH;          // (what registers hold)
 #pragma unroll
-        for (int i = 0; i < HIGH; ++i) {
-            float z[8];
-            load_chunk<Z>(a.z, row + i, col, row + i < a.rows ? n : 0, z);
-            times_slope(a.act, v[i], z);
+            for (int from = 0; from < HIGH; from += kSome) {
+                Chunk<Z> z_raw[kSome];
+#pragma unroll
+                for (int i = 0; i < kSome; ++i) fetch_chunk<Z, NARROW>(z_raw[i], a.z, min(row + from + i, a.rows - 1), col, a.cols);
+#pragma unroll
+                for (int i = 0; i < kSome; ++i) {
+                    float z[8];
+                    take_chunk<T, NARROW>(raw[from + i], there(from + i), v[from + i]);
+                    take_chunk<Z, NARROW>(z_raw[i], there(from + i), z);
+                    times_slope(a.act, v[from + i], z);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < HIGH; ++i) take_chunk<T, NARROW>(raw[i], there(i), v[i]);
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < HIGH; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
     }
     // largest magnitudes: of a row's group in `own`, of the thread's rows in each column; a value that is not finite shows in them
     float own[HIGH], down_top[8];
@@ -229,13 +250,16 @@ void save(const BlockSave& a, hipStream_t s) {
     const dim3 grid((unsigned)blocks);
     const int type = a.out.p ? a.out.kind : a.out_t.kind;
     constexpr int kMany = kAcross * kBlock / 8, kFew = kAcross * kBlock / 4;
-    if (blocks <= kFewBlocks) {
-        if (type == E4M3_TILES) k_block_save<T, Z, true, 4><<<grid, kFew, 0, s>>>(a, blocks_x);
-        else k_block_save<T, Z, false, 4><<<grid, kFew, 0, s>>>(a, blocks_x);
-    } else {
-        if (type == E4M3_TILES) k_block_save<T, Z, true, 8><<<grid, kMany, 0, s>>>(a, blocks_x);
-        else k_block_save<T, Z, false, 8><<<grid, kMany, 0, s>>>(a, blocks_x);
+    // (tiles are weights': nothing is multiplied by a slope on the way to them)
+    const auto start = [&](auto tiles) {
+        if (a.cols < kChunk) k_block_save<T, Z, tiles(), 4, true><<<grid, kFew, 0, s>>>(a, blocks_x);
+        else if (blocks <= kFewBlocks) k_block_save<T, Z, tiles(), 4><<<grid, kFew, 0, s>>>(a, blocks_x);
+        else k_block_save<T, Z, tiles(), 8><<<grid, kMany, 0, s>>>(a, blocks_x);
+    };
+    if constexpr (Z == NONE_KIND) {
+        if (type == E4M3_TILES) return start(std::true_type());
     }
+    start(std::false_type());
 }
 template <int FROM, int TO>
 hipError_t load(int rows, int cols, const Mat& in, const Mat& out, hipStream_t s) {

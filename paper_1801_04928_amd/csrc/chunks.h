@@ -202,14 +202,16 @@ template <int KIND> struct Chunk;
 template <> struct Chunk<F32> { v4f a[2]; };
 template <> struct Chunk<BF16> { v4u a; };
 template <> struct Chunk<E4M3> { v2u a; int byte; };
+template <> struct Chunk<E4M3_128> { v2u a; int byte; };
 
 // Chunk of the row (which is there) from column col on; cols: the matrix's columns.
 template <int KIND, bool NARROW>
 __device__ __forceinline__ void fetch_chunk(Chunk<KIND>& c, const Mat& m, long long row, int col, int cols) {
-    if constexpr (KIND == E4M3) {
-        const int at = min(col, (cols - 1) / kGroup * kGroup + (kGroup - kChunk));
+    if constexpr (KIND == E4M3 || KIND == E4M3_128) {
+        constexpr int kOf = kGroupOf<KIND>;
+        const int at = min(col, (cols - 1) / kOf * kOf + (kOf - kChunk));
         c.a = *as_global<const v2u>((const uint8_t*)m.p + row * m.ld + at);
-        c.byte = *as_global<const uint8_t>(m.scales + row * m.scale_ld + at / kGroup);
+        c.byte = *as_global<const uint8_t>(m.scales + row * m.scale_ld + at / kOf);
     } else {
         typedef typename Stored<KIND>::type T;
         const T* p = (const T*)m.p + row * m.ld;
@@ -239,12 +241,15 @@ __device__ __forceinline__ void fetch_chunk(Chunk<KIND>& c, const Mat& m, long l
 // Its values; n (0..8) of them are in the row, the others are zero.
 template <int KIND, bool NARROW>
 __device__ __forceinline__ void take_chunk(Chunk<KIND> c, int n, float (&v)[8]) {
-    if (n < kChunk) {
-        if constexpr (KIND == E4M3) keep_codes(c.a, n);
-        else if constexpr (!NARROW) shift_down(c.a, kChunk - max(n, 0));
+    if constexpr (KIND != E4M3 && KIND != E4M3_128) {
+        if (n < kChunk && (!NARROW || n <= 0)) shift_down(c.a, kChunk - max(n, 0));
     }
-    if constexpr (KIND == E4M3) {
+    if constexpr (KIND == E4M3 || KIND == E4M3_128) {
         eight_values(c.a, scale_value(c.byte), v);
+        if (n < kChunk) {                                  // (the scale may be no number)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.0f;
+        }
     } else if constexpr (KIND == F32) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { v[i] = c.a[0][i]; v[4 + i] = c.a[1][i]; }

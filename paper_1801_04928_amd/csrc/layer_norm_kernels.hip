@@ -168,7 +168,7 @@ struct Backward {
 // The gradients of gain and shift for 64 columns, over all rows, by a whole block of THREADS: eight threads hold the columns' chunks, and every
 // THREADS / 8-th row is a thread's.  For few rows, whose dy and s are read once more for it: that costs less than another launch.
 constexpr int kStripCols = 64;
-template <int T, int S, int THREADS>
+template <int T, int S, int THREADS, bool NARROW>
 __device__ __forceinline__ void strip_gradients(const Backward& a, float* dgain, float* dshift, int strip) {
     constexpr int kWays = THREADS / 8, kWaves = THREADS / kWave, kSome = 4;
     __shared__ float sums[kWaves][2][kStripCols];
@@ -176,23 +176,29 @@ __device__ __forceinline__ void strip_gradients(const Backward& a, float* dgain,
     float total[2][8] = {};
 #pragma unroll 1
     for (int row0 = threadIdx.x / 8; row0 < a.rows; row0 += kWays * kSome) {
-        float dy[kSome][8], h[kSome][8], rstd[kSome], mean[kSome];
+        // (past the last row it is loaded again: a branch would have each load waited for by itself)
+        Chunk<T> dy_raw[kSome];
+        Chunk<S> s_raw[kSome];
+        float rstd[kSome], mean[kSome];
 #pragma unroll
         for (int u = 0; u < kSome; ++u) {
-            const int row = row0 + u * kWays, there = row < a.rows ? n : 0;
-            load_chunk<T>(a.dy, row, col, there, dy[u]);
-            load_chunk<S>(a.sum, row, col, there, h[u]);
-            rstd[u] = a.rstd[min(row, a.rows - 1)];
-            mean[u] = a.mean[min(row, a.rows - 1)];
+            const int row = min(row0 + u * kWays, a.rows - 1);
+            fetch_chunk<T, NARROW>(dy_raw[u], a.dy, row, col, a.cols);
+            fetch_chunk<S, NARROW>(s_raw[u], a.sum, row, col, a.cols);
+            rstd[u] = a.rstd[row];
+            mean[u] = a.mean[row];
         }
 #pragma unroll
         for (int u = 0; u < kSome; ++u) {
-            const bool there = row0 + u * kWays < a.rows;
+            const int there = row0 + u * kWays < a.rows ? n : 0;
+            float dy[8], h[8];
+            take_chunk<T, NARROW>(dy_raw[u], there, dy);
+            take_chunk<S, NARROW>(s_raw[u], there, h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 // (what is not there has no part in it, whatever lies in the statistics that were read for it)
-                total[0][i] = fmaf(dy[u][i], there && i < n ? (h[u][i] - mean[u]) * rstd[u] : 0.0f, total[0][i]);
-                total[1][i] += dy[u][i];
+                total[0][i] = fmaf(dy[i], i < there ? (h[i] - mean[u]) * rstd[u] : 0.0f, total[0][i]);
+                total[1][i] += dy[i];
             }
         }
     }
@@ -216,19 +222,19 @@ __device__ __forceinline__ void strip_gradients(const Backward& a, float* dgain,
     if (out && at < a.cols) out[at] = v;
 }
 
-// A few rows: a row at a time and no sums over them, which blocks of their own take at the same time (strip_gradients).  333 x 4100 fp32 10.5 us,
-// a load, a reduction and a store one after the other; with partial sums and a launch that ends them 17.
+// A few rows: a row at a time and no sums over them, which blocks of their own take at the same time (strip_gradients).  333 x 4100 fp32 9.4 us,
+// 6.3 without the strips; with partial sums and a launch that ends them 17.
 template <int T, int S, int TPR, int NCH, bool NARROW>
-__global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_layer_backward_few(const Backward a, int row_blocks, float* dgain, float* dshift) {
+__global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_layer_backward_few(const Backward a, int strips, float* dgain, float* dshift) {
     constexpr int kBlockThreads = TPR > kThreads ? TPR : kThreads, kRows = kBlockThreads / TPR;
-    if ((int)blockIdx.x >= row_blocks) {
-        strip_gradients<T, S, kBlockThreads>(a, dgain, dshift, (int)blockIdx.x - row_blocks);
+    if ((int)blockIdx.x < strips) {                        // (they take longer than the rows)
+        strip_gradients<T, S, kBlockThreads, NARROW>(a, dgain, dshift, (int)blockIdx.x);
         return;
     }
     __shared__ float shared[2][2][TPR > kWave ? TPR / kWave : 1];
     int place = 0;
     const int t = threadIdx.x % TPR, mine = kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
-    const long long row = (long long)blockIdx.x * kRows + mine;
+    const long long row = (long long)((int)blockIdx.x - strips) * kRows + mine;
     if (row >= a.rows) return;                              // (with several rows a block there is no barrier)
     const bool more = a.dsum.p != nullptr;
     const auto col_of = [&](int j) { return (j * TPR + t) * kChunk; };
@@ -434,11 +440,16 @@ __global__ __launch_bounds__(kThreads) void k_layer_gradients(const Backward a, 
     const int col = (blockIdx.x * kStripChunks + t) * kChunk, n = a.cols - col;
     const int first = blockIdx.y * rows_per_block, end = min(a.rows, first + rows_per_block);
     float total[2][8] = {};
+#pragma unroll 2
     for (int row = first + mine; row < end; row += kStripRows) {
+        Chunk<T> dy_raw;
+        Chunk<S> s_raw;
         float dy[8], h[8];
-        load_chunk<T>(a.dy, row, col, n, dy);
-        load_chunk<S>(a.sum, row, col, n, h);
+        fetch_chunk<T, false>(dy_raw, a.dy, row, col, a.cols);      // (rows of many columns)
+        fetch_chunk<S, false>(s_raw, a.sum, row, col, a.cols);
         const float rstd = a.rstd[row], mean = a.mean[row];
+        take_chunk<T, false>(dy_raw, n, dy);
+        take_chunk<S, false>(s_raw, n, h);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             total[0][i] = fmaf(dy[i], i < n ? (h[i] - mean) * rstd : 0.0f, total[0][i]);
@@ -519,9 +530,8 @@ hipError_t forward_of(const Forward& a, hipStream_t s) {
 // kernel of their own.  (16384 x 16384 bf16 in one, with 156 registers spilled: 1054 us.)
 constexpr int kThreadsWithSums = 512, kColsWithSums = 8192;
 // A few rows: the second reading of dy and s, of matrices that lie in the caches, costs less than the launch that ends partial sums (us, this
-// way | with partial sums: 256 x 1000 fp32 8.3 | 11.4, 500 x 8192 bf16 15.0 | 22.5, 512 x 16384 fp32 37 | 43).  Of s in 8 bits it takes longer, which shows
-// where a block has fewer than 512 threads: 256 x 1000 9.4 | 11.7, 400 x 1000 14.1 | 11.8.
-bool few(int rows, int cols, bool eight) { return cols <= kHeldCols && rows <= (eight && cols <= 4096 ? 256 : 512); }
+// way | with partial sums: 256 x 1000 fp32 8.3 | 11.4, 500 x 8192 bf16 10.6 | 22.5, 1000 x 8192 fp32 30 | 42, 1000 x 4096 19 | 20; but 1000 x 1000 16 | 12).
+bool few(int rows, int cols) { return cols <= kHeldCols && rows <= (cols >= 4096 && cols <= kColsWithSums ? 1024 : 512); }
 
 template <int T, int S>
 hipError_t backward_few(const Backward& a, float* dgain, float* dshift, hipStream_t s) {
@@ -529,7 +539,7 @@ hipError_t backward_few(const Backward& a, float* dgain, float* dshift, hipStrea
         if constexpr (!again()) {
             constexpr int block = tpr() > kThreads ? tpr() : kThreads;
             const int rows = ceil_div(a.rows, block / tpr()), strips = dgain || dshift ? ceil_div(a.cols, kStripCols) : 0;
-            k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(rows + strips), block, 0, s>>>(a, rows, dgain, dshift);
+            k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(strips + rows), block, 0, s>>>(a, strips, dgain, dshift);
         }
         return hipGetLastError();
     });
@@ -542,7 +552,7 @@ hipError_t backward(const Backward& a, hipStream_t s) {
         if constexpr (again()) {
             k_layer_backward<T, S, tpr(), nch(), true, narrow()><<<dim3(std::min(a.rows, kMostGroups)), block, 0, s>>>(a);
         } else if constexpr (tpr() > kThreadsWithSums) {
-            k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(a.rows), block, 0, s>>>(a, a.rows, nullptr, nullptr);
+            k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(a.rows), block, 0, s>>>(a, 0, nullptr, nullptr);
         } else {
             k_layer_backward<T, S, tpr(), nch(), false, narrow()><<<dim3(parts), block, 0, s>>>(a);
         }
@@ -562,7 +572,7 @@ hipError_t launch_layer_norm_forward(int rows, int cols, const Mat& x, const Mat
 }
 
 int layer_norm_partials(int rows, int cols) {
-    if (rows == 0 || few(rows, cols, true)) return 0;         // (what any type needs)
+    if (rows == 0 || few(rows, cols)) return 0;
     if (cols > kColsWithSums) return std::min(ceil_div(rows, 16), 64);
     return std::min(ceil_div(rows, rows_per_block(cols)), 512);
 }
@@ -573,7 +583,7 @@ hipError_t launch_layer_norm_backward(int rows, int cols, const Mat& dy, const M
     if (rows > 0) {
         const Backward a{rows, cols, dy, sum, dsum, dx, gain, mean, rstd, dgain || dshift ? partial : nullptr};
         hipError_t e;
-        if (few(rows, cols, sum.kind == E4M3)) {
+        if (few(rows, cols)) {
             if (dy.kind == F32) return sum.kind == E4M3 ? backward_few<F32, E4M3>(a, dgain, dshift, s) : backward_few<F32, F32>(a, dgain, dshift, s);
             return sum.kind == E4M3 ? backward_few<BF16, E4M3>(a, dgain, dshift, s) : backward_few<BF16, BF16>(a, dgain, dshift, s);
         }
