@@ -440,7 +440,6 @@ __global__ __launch_bounds__(kThreads) void k_layer_gradients(const Backward a, 
     const int col = (blockIdx.x * kStripChunks + t) * kChunk, n = a.cols - col;
     const int first = blockIdx.y * rows_per_block, end = min(a.rows, first + rows_per_block);
     float total[2][8] = {};
-#pragma unroll 2
     for (int row = first + mine; row < end; row += kStripRows) {
         Chunk<T> dy_raw;
         Chunk<S> s_raw;
