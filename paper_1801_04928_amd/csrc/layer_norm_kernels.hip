@@ -543,6 +543,16 @@ hipError_t backward_few(const Backward& a, float* dgain, float* dshift, hipStrea
         return hipGetLastError();
     });
 }
+// `rows` rows from `first` on.
+Mat rows_of(Mat m, long long first) {
+    if (m.p) m.p = (uint8_t*)m.p + first * m.ld * (m.kind == F32 ? 4 : m.kind == BF16 ? 2 : 1);
+    if (m.scales) m.scales += first * m.scale_ld;
+    return m;
+}
+Backward rows_of(const Backward& a, int first, int rows) {
+    return Backward{rows, a.cols, rows_of(a.dy, first), rows_of(a.sum, first), rows_of(a.dsum, first), rows_of(a.dx, first),
+                    a.gain, a.mean + first, a.rstd + first, a.partial};
+}
 template <int T, int S>
 hipError_t backward(const Backward& a, hipStream_t s) {
     return by_width(a.cols, [&](auto tpr, auto nch, auto again, auto narrow) {
@@ -551,7 +561,12 @@ hipError_t backward(const Backward& a, hipStream_t s) {
         if constexpr (again()) {
             k_layer_backward<T, S, tpr(), nch(), true, narrow()><<<dim3(std::min(a.rows, kMostGroups)), block, 0, s>>>(a);
         } else if constexpr (tpr() > kThreadsWithSums) {
-            k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(a.rows), block, 0, s>>>(a, 0, nullptr, nullptr);
+            for (int first = 0; first < a.rows; first += kMostGroups) {      // (a workgroup a row)
+                const Backward part = rows_of(a, first, std::min(a.rows - first, kMostGroups));
+                k_layer_backward_few<T, S, tpr(), nch(), narrow()><<<dim3(part.rows), block, 0, s>>>(part, 0, nullptr, nullptr);
+                const hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
         } else {
             k_layer_backward<T, S, tpr(), nch(), false, narrow()><<<dim3(parts), block, 0, s>>>(a);
         }

@@ -60,3 +60,22 @@ def test_distillation():
     n, short = P.Distillation(rows, classes, top, temperature=2.0), P.Distillation(last, classes, top, temperature=2.0)
     loss, want = n.forward(z, t, k), short.forward(z[-last:], t[-last:], k[-last:])
     assert torch.equal(loss[-last:], want) and torch.equal(n.dlogits[-last:], short.dlogits)
+
+
+def test_layer_norm_backward_of_more_rows_than_a_launch_takes():
+    """A workgroup a row, 2^20 of them a launch: the rows at the borders of the launches, of a sum in either form."""
+    torch.cuda.empty_cache()
+    part, cols = 1 << 20, 8193
+    rows = 4 * part + 3
+    x = noise(rows, cols, 9)                                 # (both the gradient and the sum)
+    mean, rstd = torch.randn(rows, device=DEV), torch.rand(rows, device=DEV)
+    m = P.E4M3Matrix(rows, cols, device=DEV).save(x)
+    at = torch.tensor([0, 1, *(i * part + j for i in (1, 2, 3, 4) for j in (-2, -1, 0, 1)), rows - 1], device=DEV)
+    n, short = P.LayerNorm(rows, cols, passes="backward"), P.LayerNorm(len(at), cols, passes="backward")
+    for stored, few in ((x, x[at]), (m, P.E4M3Matrix.of(m.codes[at], m.scales[at], cols))):
+        n._dx.fill_(77)
+        dx = n.backward(x, stored=stored, mean=mean, rstd=rstd)
+        assert torch.equal(dx[at], short.backward(x[at], stored=few, mean=mean[at], rstd=rstd[at]))
+        assert all(not bool((v == 77).all(1).any()) for v in dx.split(part))
+    del x, m, n, dx, stored
+    torch.cuda.empty_cache()
