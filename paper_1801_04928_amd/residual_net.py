@@ -98,6 +98,8 @@ class ResidualNet:
             for p, w, bias in self._products:
                 p.set_params(w, bias)
         self._masters, self._losses = None, {}
+        # whether a replay has filled the weights' fp32 copies, where a captured step was the first (None: no such step)
+        self._filled, self._unfilled = None, torch.zeros((), dtype=torch.bool, device=device)
         self.gain = [n.gain for n in self.norms]
         self.shift = [n.shift for n in self.norms] if self._layer else []
         if self._both:
@@ -178,21 +180,35 @@ class ResidualNet:
         self.backward(loss.dlogits)
         return rows
 
+    def _capturing(self) -> bool:
+        """Whether what is enqueued now goes into a HIP graph."""
+        cuda, device = self.torch.cuda, self.w1[0].device
+        if device.type != "cuda":
+            return False
+        with cuda.device(device):
+            return cuda.is_current_stream_capturing()
+
     def descend(self, eta: float) -> None:
         """A plain gradient-descent step: every parameter less eta times its gradient.  Weights in bf16 descend in fp32 copies, made
         in the first step, and are these copies' roundings, so that steps smaller than half of bf16's add up.  A weight that was
-        set to something else meanwhile goes on from there."""
+        set to something else meanwhile goes on from there.  A step may be captured, the first among them."""
         torch = self.torch
         own = [*self.w1, *self.w2, *([self.w_out] if self.classes else [])]
         grads = [*self.dw1, *self.dw2, *([self.dw_out] if self.classes else [])]
         if self.dtype == torch.float32:
             weights = own
         else:
-            if self._masters is None:
+            if self._masters is None and self._capturing():
+                # (a copy that is captured would be made again in every replay: these are filled by the first)
+                self._masters, self._filled = [torch.empty_like(w, dtype=torch.float32) for w in own], self._unfilled
+            elif self._masters is None:
                 self._masters = [w.float() for w in own]
             weights = self._masters
             for w, master in zip(own, weights):
-                master.copy_(torch.where(master.to(w.dtype) == w, master, w.float()))
+                same = master.to(w.dtype) == w
+                if self._filled is not None:
+                    same &= self._filled
+                master.copy_(torch.where(same, master, w.float()))
         vectors = [*self.b1, *self.b2, *self.gain, *self.shift, *([self.b_out] if self.classes else [])]
         vector_grads = [*self.db1, *self.db2, *self.dgain, *self.dshift, *([self.db_out] if self.classes else [])]
         for p, g in zip((*weights, *vectors), (*grads, *vector_grads)):
@@ -200,4 +216,6 @@ class ResidualNet:
         for w, master in zip(own, weights):
             if master is not w:
                 w.copy_(master)
+        if self._filled is not None:
+            self._filled.fill_(True)
         self._stale = self._blocks
