@@ -648,6 +648,10 @@ class BlockLinear(_Operator):
         """Register w ([outputs][inputs], f32 or bf16) and b ([outputs] f32, or None), and keep w in 8 bits.  w and b are kept by reference:
         after w has changed, `refresh`.  w may be in 8 bits already, an E4M3Blocks with tiles; the backward pass needs w_t then, its
         transposed."""
+        self._register(w, b, w_t)
+        self.refresh()
+
+    def _register(self, w, b=None, w_t=None) -> None:
         kept = _Kept("b", b, self.outputs, self._gpu)
         shape, gpu = (self.outputs, self.inputs), self._gpu
         if isinstance(w, E4M3Blocks):
@@ -666,7 +670,6 @@ class BlockLinear(_Operator):
                 self.w8_t = E4M3Blocks(*shape[::-1], tiles=True, device=self.device) if self._backward else None
             self.w = w
         self.b, self._kept_b = b, kept
-        self.refresh()
 
     def refresh(self) -> None:
         """Keep the weights as they are now in 8 bits.  (Weights that were given in 8 bits are read as they lie.)"""

@@ -26,7 +26,11 @@ class ResidualNet:
     Parameters, one per block: gain (f32), with norm="layer" shift (f32), w1, w2 (storage type), b1, b2 (f32); with classes
     another gain (and shift), w_out and b_out.  Their gradients: dgain, dshift, dw1, dw2, db1, db2, dw_out, db_out.  `forward(x)` gives
     the output, `backward(dy)` the gradient of x, and `distil` makes a whole pass of learning from a teacher.  With
-    products="e4m3_128" weights that are set otherwise than by `init` and `descend` need `refresh`."""
+    products="e4m3_128" weights that are set otherwise than by `init` and `descend` need `refresh`.
+
+    All calls but `init` may be captured in a HIP graph.  What a captured pass computes is of the weights at its replay, whether an eager
+    call moved them or a replayed one.  (With products="e4m3_128" a captured step puts them into 8 bits behind itself, and a pass that is
+    captured while they have moved since the last eager one also in front of itself: `refresh` before the capture saves that.)"""
 
     def __init__(self, depth: int, width: int, hidden: int, rows: int, dtype="bf16", act: str = "gelu",
                  checkpoints="storage", device: str = "cuda:0", norm: str = "rms", products: str = "storage", classes=None,
@@ -93,10 +97,10 @@ class ResidualNet:
         self._products = [*zip(self.ups, self.w1, self.b1), *zip(self.downs, self.w2, self.b2)]
         if classes is not None:
             self._products.append((self.head, self.w_out, self.b_out))
-        self._stale, self._set = self._blocks, not self._blocks
-        if not self._blocks:
-            for p, w, bias in self._products:
-                p.set_params(w, bias)
+        for p, w, bias in self._products:
+            (p._register if self._blocks else p.set_params)(w, bias)
+        # of the weights in 8 bits: the next pass has to make them; a captured pass that does not make them reads them
+        self._stale, self._relied = self._blocks, False
         self._masters, self._losses = None, {}
         # whether a replay has filled the weights' fp32 copies, where a captured step was the first (None: no such step)
         self._filled, self._unfilled = None, torch.zeros((), dtype=torch.bool, device=device)
@@ -118,20 +122,33 @@ class ResidualNet:
         for w, scale in pairs + ([(self.w_out, 1.0)] if self.classes else []):
             v = self.torch.randn(w.shape, generator=g, device=w.device)
             w.copy_(v * (scale * w.shape[1] ** -0.5))
-        self._stale = self._blocks
+        self._moved()
 
     def refresh(self) -> None:
         """Keeps the weights as they are now in 8 bits, if the products take them so."""
-        for p, w, bias in self._products if self._blocks else ():
-            if self._set:
-                p.refresh()
-            else:
-                p.set_params(w, bias)
-        self._stale, self._set = False, True
+        if not self._blocks:
+            return
+        for p, _, _ in self._products:
+            p.refresh()
+        if not self._capturing():              # (what is captured has not run)
+            self._stale = False
+
+    def _moved(self) -> None:
+        """The weights are others now.  No replay comes back to this class to ask whether they are: a captured step makes them in 8 bits
+        again, and an eager one does for the captured passes that do not."""
+        if not self._blocks:
+            return
+        capturing = self._capturing()
+        if capturing or self._relied:
+            self.refresh()
+        if not capturing:
+            self._stale = True                 # (made by the next eager pass, of what the caller sets until then, too)
 
     def forward(self, x):
         if self._stale:
             self.refresh()
+        elif self._blocks and not self._relied:
+            self._relied = self._capturing()
         s, branch = x, None
         for b in range(self.depth):
             s, h = self._normed(b, s, branch)
@@ -185,6 +202,8 @@ class ResidualNet:
         cuda, device = self.torch.cuda, self.w1[0].device
         if device.type != "cuda":
             return False
+        if cuda.current_device() == device.index:
+            return cuda.is_current_stream_capturing()
         with cuda.device(device):
             return cuda.is_current_stream_capturing()
 
@@ -218,4 +237,4 @@ class ResidualNet:
                 w.copy_(master)
         if self._filled is not None:
             self._filled.fill_(True)
-        self._stale = self._blocks
+        self._moved()

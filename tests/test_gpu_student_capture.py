@@ -8,7 +8,7 @@ from tests.student_util import DEV, TYPE, values
 
 pytestmark = pytest.mark.gpu
 ROWS, WIDTH, HIDDEN, CLASSES, TOP, T, ETA = 20, 40, 136, 45, 4, 2.0, 2.0 ** -7
-KINDS = [("f32", "storage"), ("bf16", "storage")]
+KINDS = [("f32", "storage"), ("bf16", "storage"), ("f32", "e4m3_128"), ("bf16", "e4m3_128")]
 
 
 def net(dtype, products):
@@ -119,3 +119,19 @@ def test_an_eager_pass_follows_captured_steps(dtype, products, before):
         y.zero_()
         forward.replay()
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype, products", KINDS)
+def test_weights_that_are_set_behind_an_eager_step_are_the_next_pass_s(dtype, products):
+    """... whether or not a pass was captured."""
+    mine, eager, data = net(dtype, products), net(dtype, products), batch(0, dtype)
+    mine.forward(data[0])
+    graph, y = captured(lambda: mine.forward(data[0]))
+    for k in range(2):
+        for n in (mine, eager):
+            step(n, data)
+            n.w2[1].mul_(0.5)
+        assert torch.equal(mine.forward(data[0]), eager.forward(data[0]))
+        graph.replay()
+        assert torch.equal(y, eager.forward(data[0]))
+        same_nets(mine, eager)
