@@ -101,7 +101,7 @@ class ResidualNet:
             (p._register if self._blocks else p.set_params)(w, bias)
         # of the weights in 8 bits: the next pass has to make them; a captured pass that does not make them reads them
         self._stale, self._relied = self._blocks, False
-        self._masters, self._losses = None, {}
+        self._masters = self._loss = None
         # whether a replay has filled the weights' fp32 copies, where a captured step was the first (None: no such step)
         self._filled, self._unfilled = None, torch.zeros((), dtype=torch.bool, device=device)
         self.gain = [n.gain for n in self.norms]
@@ -185,14 +185,18 @@ class ResidualNet:
     def distil(self, x, top_logits, top_classes, temperature: float = 1.0, weight=None):
         """A forward and a backward pass that learns from a teacher's top logits ([rows][top], f32 or bf16) of the classes that top_classes
         names (int32, negative: no entry): the loss of each row, f32, as `Distillation` has it.  The parameters' gradients are those
-        of the sum of the rows' losses, each times its weight ([rows] f32, None: ones).  The logits are overwritten."""
+        of the sum of the rows' losses, each times its weight ([rows] f32, None: ones).  The logits are overwritten; the losses are a
+        tensor of their own."""
         if self.classes is None or not self._both:
             raise LfError(LF_EINVAL, "distil: the net was made without classes or without its backward pass")
-        key = int(top_logits.shape[1]), float(temperature)
-        if key not in self._losses:
-            self._losses[key] = Distillation(self.rows, self.classes, key[0], self.dtype, temperature=key[1], dlogits=self.out,
-                                             device=self.w_out.device)
-        loss = self._losses[key]
+        if top_logits.dim() != 2:
+            raise LfError(LF_EINVAL, f"top_logits: a matrix is needed, got {list(top_logits.shape)}")
+        top = int(top_logits.shape[1])
+        if self._loss is None:
+            self._loss = Distillation(self.rows, self.classes, top, self.dtype, dlogits=self.out, device=self.w_out.device)
+        # (one for every temperature and number of entries)
+        loss = self._loss
+        loss.top, loss.temperature, loss._loss = top, float(temperature), self.torch.empty_like(loss._loss)
         rows = loss.forward(self.forward(x), top_logits, top_classes, weight)
         self.backward(loss.dlogits)
         return rows

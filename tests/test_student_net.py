@@ -51,3 +51,9 @@ def test_every_parameter_descends(dtype):
     for _ in range(64):
         n.descend(2.0 ** -11)
     assert all(bool((v == 1 - 2.0 ** -6).all()) for v in params) and n._stale
+
+
+def test_teachers_of_no_matrix_are_refused():
+    for t in (torch.zeros(()), torch.zeros(4), torch.zeros(4, 3, 1)):
+        with pytest.raises(P.LfError, match="top_logits"):
+            net(classes=30).distil(torch.zeros(4, 40), t, torch.zeros(4, 3, dtype=torch.int32))
