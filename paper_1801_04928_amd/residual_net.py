@@ -13,7 +13,7 @@ pass keeps the transposed codes then, whatever `checkpoints` says of s and of th
 from __future__ import annotations
 
 from .binding import LF_EINVAL, LfError
-from .operators import (BlockLinear, Distillation, E4M3Matrix, LayerNorm, Linear, RmsNorm, lf_block_linear_backward_workspace_bytes,
+from .operators import (BlockLinear, Distillation, E4M3Blocks, E4M3Matrix, LayerNorm, Linear, RmsNorm, lf_block_linear_backward_workspace_bytes,
                         lf_block_linear_workspace_bytes, lf_linear_backward_workspace_bytes, lf_linear_workspace_bytes, _storage)
 
 
@@ -68,12 +68,17 @@ class ResidualNet:
         product = BlockLinear if self._blocks else Linear
         # h and u: kept as they are; with blocks of 128 the product keeps their transposed codes, and what was put in is free again,
         # or, where there is nothing to keep, the norm and the product write the next one's operand themselves
-        if not self._blocks:
+        if self._both and not self._blocks:
             h = u = kept
         elif self._both:
             h, u = torch.empty((rows, width), **new), torch.empty((rows, hidden), **new)
         else:
-            h, u = "e4m3_128" if self._layer else self.dtype, "e4m3_128"
+            def free_again(cols, kind):
+                if kind == "e4m3":
+                    return E4M3Matrix(rows, cols, device)
+                return E4M3Blocks(rows, cols, device=device) if kind == "e4m3_128" else torch.empty((rows, cols), **new)
+            h = free_again(width, kept if not self._blocks else "e4m3_128" if self._layer else self.dtype)
+            u = free_again(hidden, "e4m3_128" if self._blocks else kept)
         z = "none" if act == "none" or not self._both else "e4m3_128" if self._blocks and kept == "e4m3" else kept
         for b in range(depth + (classes is not None)):
             # the running sum is updated in place; its checkpoint, or in the storage type the sum itself, is the block's

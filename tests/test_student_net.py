@@ -57,3 +57,11 @@ def test_teachers_of_no_matrix_are_refused():
     for t in (torch.zeros(()), torch.zeros(4), torch.zeros(4, 3, 1)):
         with pytest.raises(P.LfError, match="top_logits"):
             net(classes=30).distil(torch.zeros(4, 40), t, torch.zeros(4, 3, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("kinds", [dict(), dict(checkpoints="e4m3"), dict(products="e4m3_128")])
+def test_a_net_for_answers_has_one_block_s_activations(kinds, norm):
+    n = P.ResidualNet(5, 40, 24, 4, device="cpu", norm=norm, passes="forward", classes=30, **kinds)
+    assert len({id(m._y) for m in n.norms}) == len({id(p._y) for p in n.ups}) == len({id(p._y) for p in n.downs}) == 1
+    assert all(p._z is None for p in n.ups)
