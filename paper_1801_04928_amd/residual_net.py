@@ -220,6 +220,8 @@ class ResidualNet:
         """A plain gradient-descent step: every parameter less eta times its gradient.  Weights in bf16 descend in fp32 copies, made
         in the first step, and are these copies' roundings, so that steps smaller than half of bf16's add up.  A weight that was
         set to something else meanwhile goes on from there.  A step may be captured, the first among them."""
+        if not self._both:
+            raise LfError(LF_EINVAL, "descend: the net was made without its backward pass")
         torch = self.torch
         own = [*self.w1, *self.w2, *([self.w_out] if self.classes else [])]
         grads = [*self.dw1, *self.dw2, *([self.dw_out] if self.classes else [])]

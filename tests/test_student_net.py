@@ -65,3 +65,11 @@ def test_a_net_for_answers_has_one_block_s_activations(kinds, norm):
     n = P.ResidualNet(5, 40, 24, 4, device="cpu", norm=norm, passes="forward", classes=30, **kinds)
     assert len({id(m._y) for m in n.norms}) == len({id(p._y) for p in n.ups}) == len({id(p._y) for p in n.downs}) == 1
     assert all(p._z is None for p in n.ups)
+
+
+def test_a_net_for_answers_does_not_learn():
+    n = net(passes="forward")
+    with pytest.raises(P.LfError, match="descend"):
+        n.descend(0.5)
+    with pytest.raises(P.LfError, match="backward"):
+        n.backward(torch.zeros(4, 40, dtype=torch.bfloat16))
