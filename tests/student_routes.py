@@ -127,3 +127,46 @@ def kernels(program, cases):
         launches = [launch.split(":") for launch in line.split()]
         found.append([(*name_of(symbol), int(groups), int(threads)) for symbol, groups, threads in launches])
     return found
+
+
+# Backward passes of products that take every way that a pass may go, each with ends in every direction: (rows, outputs, inputs), and the launches
+# that follow the one that makes dz and db's partial sums, tiles and splits of dx and of dw among them.  The sizes follow from the choice of
+# the tiles; where that changes, they do.
+BACKWARD = [
+    ((17, 8200, 2100), ["both 128, dx split", "join"]), ((3000, 130, 3333), ["both 128, dw split", "join"]),
+    ((3000, 3333, 130), ["both 128, dx split, dw split", "join"]), ((300, 1100, 2050), ["both 128"]),
+    ((3, 8190, 8187), ["dx few", "dw 256"]), ((2100, 5003, 2050), ["join", "dx 128", "dw 256"]), ((3001, 2050, 4100), ["join", "dx 256", "dw 256"]),
+    ((9000, 2050, 2050), ["join", "dx 128", "dw 256, split", "join"]),
+]
+
+
+def describe_backward(sizes, launches):
+    """The launches of a whole backward pass behind the first."""
+    rows, outputs, inputs = sizes
+
+    def tiles(use, tile):
+        m, n = (rows, inputs) if use == "dx" else (outputs, inputs)
+        return -(-m // tile) * -(-n // tile)
+    assert launches[0][0] == "k_block_save"
+    found, uses = [], iter(("dx", "dw"))
+    for kernel, args, groups, _ in launches[1:]:
+        if kernel == "k_block_join":
+            found.append("join")
+        elif kernel == "k_block_few":
+            found.append(f"{next(uses)} few")
+        elif kernel == "k_block_product":
+            use = next(uses)
+            found.append(f"{use} {args[0]}" + ", split" * (groups > tiles(use, args[0])))
+        else:                              # (the workgroups of both products and, 512 columns each, of db's sums over more than 128 rows)
+            assert kernel == "k_block_both"
+            rest, x, w = groups - (-(-outputs // 512) if rows > 128 else 0), tiles("dx", 128), tiles("dw", 128)
+            ways = [(i, j) for i in range(1, 257) for j in range(1, 257) if i * x + j * w == rest]
+            assert ways
+            found.append(f"both {args[0]}" + (", dx split" * all(i > 1 for i, _ in ways) + ", dw split" * all(j > 1 for _, j in ways)))
+    return found
+
+
+# Layer norms' backward passes over many rows, by the kernel that they take beside those of tests/test_gpu_layer_norm.py: (rows, columns).
+NORM_BACK = {"k_layer_backward, 64 threads": [(1300, 1023)], "k_layer_backward, 256 threads": [(700, 2500), (1100, 4095)],
+             "k_layer_backward, 512 threads": [(1030, 5000), (1100, 8191)], "k_layer_backward_few, 512 threads": [(1024, 4097)],
+             "k_layer_gradients, 256 threads": [(600, 9001)]}

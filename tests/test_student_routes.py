@@ -27,3 +27,20 @@ def test_grids_have_fewer_than_2_to_the_32_threads(program):
             cases += [("product_back", rows_along, cols, inputs, type_, wanted) for inputs in (1, 129, 8192) for wanted in ("dx", "dw", "all")]
     wrong = [(case, k) for case, launches in zip(cases, R.kernels(program, cases)) for k in launches if k[2] * k[3] >= 1 << 32]
     assert not wrong, "\n".join(map(str, wrong))
+
+
+def test_backward_passes_of_products_go_the_ways_they_name(program):
+    for type_ in ("bf16", "f32"):
+        cases = [("product_back", *sizes, type_, "all") for sizes, _ in R.BACKWARD]
+        got = [(sizes, R.describe_backward(sizes, k)) for (sizes, _), k in zip(R.BACKWARD, R.kernels(program, cases))]
+        assert got == R.BACKWARD
+
+
+def test_layer_norms_take_the_kernels_they_name(program):
+    for type_ in ("bf16", "f32"):
+        for kept in ("-", "e4m3"):
+            for want, sizes in R.NORM_BACK.items():
+                for launches in R.kernels(program, [("norm_back", *s, type_, kept, "all") for s in sizes]):
+                    named = [f"{kernel}, {threads if kernel != 'k_layer_backward' else args[2]} threads" for kernel, args, _, threads in launches]
+                    assert want in named, (want, sizes, named)
+                    assert ("k_layer_finish, 1024 threads" in named) == ("few" not in want)
