@@ -167,6 +167,6 @@ def describe_backward(sizes, launches):
 
 
 # Layer norms' backward passes over many rows, by the kernel that they take beside those of tests/test_gpu_layer_norm.py: (rows, columns).
-NORM_BACK = {"k_layer_backward, 64 threads": [(1300, 1023)], "k_layer_backward, 256 threads": [(700, 2500), (1100, 4095)],
+NORM_BACK = {"k_layer_backward, 64 threads": [(1300, 1023), (1300, 5)], "k_layer_backward, 256 threads": [(700, 2500), (1100, 4095)],
              "k_layer_backward, 512 threads": [(1030, 5000), (1100, 8191)], "k_layer_backward_few, 512 threads": [(1024, 4097)],
              "k_layer_gradients, 256 threads": [(600, 9001)]}

@@ -56,6 +56,29 @@ def test_products(rows, outputs, inputs, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dz_of_many_blocks_from_z_in_8_bits(dtype):
+    """648 blocks of 128 x 128, which eight rows a thread take."""
+    rows, outputs, inputs = 3000, 3333, 130
+    dy, z = values(3, rows, outputs, dtype=dtype, std=0.01), values(4, rows, outputs, dtype=dtype)
+    x = values(1, rows, inputs, dtype=dtype)
+    mdy, mz, mx = Dense(rows, outputs, dtype, dy, 1, 2), Blocks(rows, outputs, values=z, pad_groups=1), Blocks(inputs, rows, values=x.t().contiguous())
+    dw, db = Dense(outputs, inputs, dtype, None, 1, 3), torch.full((outputs + 1,), MARK, device=DEV)
+    nbytes = P.lf_block_linear_backward_workspace_bytes(rows, outputs, inputs)
+    scratch = torch.full((nbytes + 256,), 255, dtype=torch.uint8, device=DEV)
+    assert P.lf_block_linear_backward(rows, outputs, inputs, mdy.m, mz.m, P.LF_ACT_RELU, mx.m, None, None, dw.m, db.data_ptr(), scratch.data_ptr(),
+                                      nbytes) == P.LF_OK
+    torch.cuda.synchronize()
+    assert bool((scratch[nbytes:] == 255).all()) and float(db[outputs]) == MARK
+    with torch.device(DEV):
+        dz = dy.to(DEV) * R.slope(R.held(z.to(DEV)), "relu")
+        want = on_cpu(R.product(R.held(dz.t().contiguous()), R.held(x.t().contiguous().to(DEV)), dtype == "f32"))
+        want_db = on_cpu((dz.sum(0), (rows + 40) * R.U * dz.abs().sum(0)))
+    dw.get()
+    near_rounded("dw", dw.t, *want)
+    near("db", db[:outputs], *want_db)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kept", ["storage", "e4m3"])
 @pytest.mark.parametrize("rows, cols", [s for sizes in NORM_BACK.values() for s in sizes])
 def test_layer_norms(rows, cols, kept, dtype):
