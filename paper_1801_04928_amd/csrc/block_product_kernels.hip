@@ -458,7 +458,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_block_join(const Join x, uns
 // ================================================================================================
 // a few rows
 // ================================================================================================
-// Up to 16 MT rows: the product is the reading of Q (1 x 8192 x 8192 bf16 14.4 us with the launch, 4.7 TB/s).  A workgroup takes 16 outputs, each of its WAVES waves every WAVES-th group of 128 of the
+// Up to 16 MT rows: the product is the reading of Q (1 x 4096 x 4096 bf16 5.8 us with the call, 1 x 8192 x 8192 16.7 = 4.0 TB/s).  A workgroup takes 16 outputs, each of its WAVES waves every WAVES-th group of 128 of the
 // contraction: a lane has 2 x 16 bytes of its output's row (and of its sample's), which the matrix instruction takes as they come, for
 // operands of one order of q on both sides.  All loads of some groups are under way at once, without a branch: past the last
 // group it is loaded again, and its codes made zeros.
@@ -607,10 +607,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_few(const Args g) {
         for (int i = 0; i < 8; ++i) v[i] += sums[w][m][col + i];
     finish_chunk(g.f, g.M, g.N, m, n0 + col, v, bias, residual);
 }
-// The same of a dense P that is small, GROUPS groups at most: the workgroup puts all of it into 8 bits in LDS first, four lanes a group, while
-// the first of Q is on its way.  Rows in LDS are 16 bytes longer than their codes, so that the rows' pieces lie in different banks.
-// 1 x 4096 x 4096 bf16 7.2 us with the launch, 1 x 8192 x 8192 14.8 = 4.5 TB/s (each wave putting the groups it multiplies into 8 bits:
-// 9.3, 26.7: sixteen lanes do the same for one row, and registers hold less of Q meanwhile).
+// The same of a dense P that is small, GROUPS groups at most: the workgroup puts all of it into 8 bits in LDS first, four lanes a group.  Rows
+// in LDS are 16 bytes longer than their codes, so that the rows' pieces lie in different banks.  1 x 4096 x 4096 bf16 6.4 us with the call (7.0
+// with silu and a residual), 1 x 8192 x 8192 14.1 = 4.8 TB/s (each wave putting the groups it multiplies into 8 bits: 9.3, 26.7: sixteen lanes do
+// the same for one row, and registers hold less of Q meanwhile).  The first of Q is asked for ahead of P, and so are bias and residual: loads
+// return in order, so what waits for P has waited for these, and the work on P overlaps with nothing.
 constexpr int kStagedWaves = 8;
 template <int XK, int MT, int GROUPS, bool EXACT>
 __global__ __launch_bounds__(64 * kStagedWaves) void k_block_few_staged(const Args g) {
@@ -719,8 +720,11 @@ constexpr int kLeastTiles = 2;           // of the contraction a split has
 
 // Measured: a tile of 128 x 128 takes 2.5 us for its start and end and 3.6 for each 1024 of the contraction where few of them run (128 x
 // 4096 x 4096: 17 us without the launch) and 5.1 where the chip is full of them (1024 x 4096 x 4096: 23); one of 256 x 256 10.5, and 8.5 to 12.2
-// (2048 x 2048 x 8192: 82, 4096 x 4096 x 8192: 108).  So the large win once they fill the chip (4096 x 4096 x 4096: 65 us against 94), the small
-// below (2048 x 2048 x 2048: 16 against 32).  What splits store and a launch reads again costs 2 us and 1 for each 4 MB.
+// (2048 x 2048 x 8192, not split: 82, 4096 x 4096 x 8192: 108).  So the large win once they fill the chip (4096 x 4096 x 4096: 64 us against 91), the
+// small below (2048 x 2048 x 2048: 15 against 31).  What splits store and a launch reads again costs 2 us and 1 for each 4 MB.
+// These are prices of the instructions for 8 bits.  Results in fp32 go by them too, whose tiles take longer: 128 x 128 | 256 x 256, the one taken
+// named first or second, 1024 x 4096 x 4096 42 | 137 (first), 2048 x 2048 x 2048 25 | 75 (first), 2048 x 2048 x 8192 74 | 97 (first), but 4096 x 4096 x
+// 4096 139 | 147 (second), 4096 x 4096 x 8192 260 | 277 (second): up to 7 % are lost.
 Plan plan_with(int tile, int M, int N, int K) {
     const double start = tile == 128 ? 2.5 : 10.5, alone = tile == 128 ? 3.6 : 8.5, crowded = tile == 128 ? 5.1 : 12.2;      // us, per 1024
     const int k_tiles = ceil_div(K, kBlock);
@@ -741,9 +745,10 @@ Plan plan_of(int M, int N, int K) {
     const Plan small = plan_with(128, M, N, K), large = plan_with(256, M, N, K);
     return large.us < small.us ? large : small;
 }
-// Up to 64 rows may also go a workgroup for 16 outputs and all of the contraction (below the tiles' kernels).  Measured: 0.8 us and, for each 1024
-// of the contraction, 0.53 and 0.033 a row, for as many workgroups as fill the chip (8 x 4096 x 4096: 3.5 us against 8 by tiles; 64 x 4096 x 4096: 11.9
-// against 10.1; 64 x 8192 x 8192: 52 against 16).
+// Up to 64 rows may also go a workgroup for 16 outputs and all of the contraction (k_block_few).  Measured: 0.8 us and, for each
+// 1024 of the contraction, 0.53 and 0.033 a row, for as many workgroups as fill the chip.  x in 8 bits, us with the call, this way | by tiles, bf16:
+// 1 x 4096 x 4096 5.8 | 10.6, 16 x 4096 x 4096 8.0 | 13.3, 64 x 2048 x 2048 8.3 | 12.2, 64 x 4096 x 4096 15.6 | 14.7, 64 x 8192 x 8192 54 | 20.5; fp32, which
+// goes by the same prices: 6.3 | 13.0, 8.0 | 15.2, 8.5 | 13.7, 15.6 | 17.9, 54 | 27.  So of fp32 64 x 4096 x 4096, sent to the tiles, loses 2 of 18 us.
 double few_us(int M, int N, int K) {
     const int groups = ceil_div(N, kFewOutputs);
     return ceil_div(groups, kGroups) * (0.8 + (0.53 + 0.033 * M) * ceil_div(K, kBlock) * kBlock / 1024);
@@ -774,8 +779,10 @@ void few(const Args& a, hipStream_t s) {
     else if (a.M <= 32) few_with<2, EXACT>(a, s);
     else few_with<4, EXACT>(a, s);
 }
-// Groups that a dense P may have.  Every workgroup puts all of them into 8 bits: from some on that takes longer than a launch that does it once (45
-// x 1365 x 1083 fp32, 405 groups, 13.5 us against 11.2).
+// Groups that a dense P may have: what LDS is laid out for.  Every workgroup puts all of them into 8 bits, and from some on that takes longer than a
+// launch that does it once: us with the call, this way | by a launch, bf16: 8 x 4096 x 4096 (256 groups) 7.5 | 10.8, 64 x 512 x 512 (256) 7.8 | 9.2,
+// 16 x 4096 x 4096 (512) 9.7 | 11.8, 32 x 2048 x 2048 (512) 9.7 | 13.0; fp32: 9.6 | 10.5, 10.1 | 9.4, 13.0 | 11.7, 13.4 | 13.1, and 45 x 1365 x 1083
+// (405) 13.5 | 11.2.  So bf16 gains at the limits, and fp32, to which they apply too, loses up to 1.3 us there.
 int staged_groups(int M) { return M <= 32 ? 512 : 256; }
 template <int XK, bool EXACT>
 void few_staged(const Args& a, hipStream_t s) {

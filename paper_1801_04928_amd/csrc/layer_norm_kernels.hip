@@ -1,6 +1,6 @@
 // The layer norm with the residual's addition, and its backward pass.  Bound by memory: every value is read once, held in registers,
-// and written once.  16384 x 8192 bf16, four matrices of it: forward 189 us, 5.7 TB/s, backward 199 us, 5.4 TB/s, where a copy of 1 GiB reaches
-// 5.1; small ones take the call's time on the host (1 x 1024 9 us, the kernel 3.4 of it).
+// and written once.  16384 x 8192 bf16, four matrices of it: forward 190 us, 5.7 TB/s, backward 200 us, 5.4 TB/s (fp32 406 and 405), where a copy of 1
+// GiB reaches 5.1 and kernels that only read or only write 6.3 and 5.7; small ones take the call's time on the host (1 x 1024 9 us, the kernel 3.4 of it).
 #include "chunks.h"
 #include "column_sums.h"
 
@@ -529,7 +529,7 @@ hipError_t forward_of(const Forward& a, hipStream_t s) {
 // kernel of their own.  (16384 x 16384 bf16 in one, with 156 registers spilled: 1054 us.)
 constexpr int kThreadsWithSums = 512, kColsWithSums = 8192;
 // A few rows: the second reading of dy and s, of matrices that lie in the caches, costs less than the launch that ends partial sums (us, this
-// way | with partial sums: 256 x 1000 fp32 8.3 | 11.4, 500 x 8192 bf16 10.6 | 22.5, 1000 x 8192 fp32 30 | 42, 1000 x 4096 19 | 20; but 1000 x 1000 16 | 12).
+// way | with partial sums: 256 x 1000 fp32 8 | 11.4, 500 x 8192 bf16 10.2 | 22.5, 1000 x 8192 fp32 30 | 42, 1000 x 4096 19 | 20; but 1000 x 1000 16 | 11).
 bool few(int rows, int cols) { return cols <= kHeldCols && rows <= (cols >= 4096 && cols <= kColsWithSums ? 1024 : 512); }
 
 template <int T, int S>
