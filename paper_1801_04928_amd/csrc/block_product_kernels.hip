@@ -93,7 +93,7 @@ __device__ __forceinline__ void load_to_lds(v4i resource, unsigned voffset, unsi
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                  :
                  : "s"(lds), "v"(voffset), "s"(resource), "s"(soffset)
-                 : "m0", "memory");
+                 : "memory");
 }
 // Until at most LEFT of a wave's loads are on their way, and all waves are here.
 template <int LEFT>
@@ -129,7 +129,7 @@ __device__ __forceinline__ void load_dwords_to_lds(v4i resource, unsigned voffse
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
                  :
                  : "s"(lds), "v"(voffset), "s"(resource), "s"(soffset)
-                 : "m0", "memory");
+                 : "memory");
 }
 
 template <int BM, int BN, int WM, int WN>
